@@ -5,8 +5,10 @@
  * that was computed ahead of time and handed in (Sec. 3.3.1, "Decoupling Preemptive Routing": per token
  * the k active expert ids and their gate weights are cached - uint8 ids and bfloat16 scores in the
  * paper's storage format, App. "Efficiency Experiment Detail" - and passed to the MoE layers).
- * Because the router is frozen (App. A, the "ideal expert gradient"), backward produces gradients for
- * the expert weights and for the layer input only; the gate weights receive none.
+ * Because the router is frozen (App. A, the "ideal expert gradient"), grouter_moe_bwd produces gradients for
+ * the expert weights and for the layer input only.  For a router that is trained (expert tuning, or one that is
+ * not frozen) there are calls of their own: scores to ids and gates and back, the balance loss, the gates'
+ * gradient, and an optimizer step.
  *
  * The paper leaves the expert f_i abstract.  Here it is a bias-free SwiGLU FFN
  *      f_e(x) = ( silu(x W1_e) * (x W3_e) ) W2_e ,   silu(g) = g / (1 + exp(-g)),
@@ -53,6 +55,8 @@ enum {
 };
 
 enum { GROUTER_IDX_INT32 = 0, GROUTER_IDX_UINT8 = 1 };
+/* element types of scores, their gradients and the optimizer's tensors */
+enum { GROUTER_FP32 = 0, GROUTER_BF16 = 1, GROUTER_FP16 = 2 };
 
 /* Human-readable name of an error code (static storage, host pointer). */
 const char* grouter_strerror(int code);
@@ -219,6 +223,125 @@ int grouter_fold_groups(const int64_t* P, int E_S, int E_T, int32_t* group_of, v
 int grouter_fold_weights(const float* W_s, const int32_t* group_of, int d, int E_S, int E_T, float* out,
                          void* stream);
 
+/* ==== the router and what trains it ===================================================================
+ * Scores are a matrix [T][E] of fp32, bf16 or fp16 (GROUTER_FP32 ...) whose rows are score_ld >= E elements apart, so it
+ * may be part of a wider one; only its own elements are read.  Rows that start at multiples of 16 bytes are read faster.
+ * token_mask [T] uint8 or NULL: tokens with 0 are padding and their scores may hold anything.
+ * Limits: 1 <= k <= E <= 1024 (E <= 256 for uint8 ids), T*k < 2^31, 1 <= S <= 2^24; no two arguments may overlap.
+ */
+
+/* How gates come from scores (Eq. 2, r = g(TopK(s, k))): g a softmax over the k selected scores, the selected ones' shares
+ * of a softmax over all E, sigmoids, or sigmoids divided by their sum over the selected. */
+enum {
+    GROUTER_GATE_SOFTMAX_SELECTED = 0,
+    GROUTER_GATE_SOFTMAX_ALL = 1,
+    GROUTER_GATE_SIGMOID = 2,
+    GROUTER_GATE_SIGMOID_NORMALISED = 3
+};
+
+/* ---- scores -> expert ids and gate weights, in the layer's (and the cache's) format -------------------
+ *   topk_idx [T][k] int32 or uint8: the k largest scores of the row, largest first, the lower expert first among equal
+ *            ones.  -0 equals +0; NaN ranks with -inf (an expert closed to the token has score -inf).
+ *   gate_w   [T][k] bf16.  Computed in fp32 and rounded once.  0 where all selected scores (for SOFTMAX_ALL: all scores)
+ *            are -inf, and for padding tokens; a NaN among the scores that a gate depends on gives NaN.
+ * A padding token gets ids like any other (in [0,E) whatever its scores), so a plan can be built from them.
+ */
+int grouter_route(const void* scores, int score_dtype, int64_t score_ld, int64_t T, int E, int k, int gating,
+                  const uint8_t* token_mask, void* topk_idx, int idx_dtype, void* gate_w, void* stream);
+
+/* ---- gradient by the scores -----------------------------------------------------------------------------
+ * dscores [T][E] (rows dscore_ld >= E apart, any of the three dtypes) = the sum of
+ *   - the gates' part, where dlog_gate is given: dlog_gate [T][k] fp32 = gate * dL/dgate, the gradient by the gate's
+ *     logarithm (what grouter_gate_bwd and grouter_moe_gate_bwd give), topk_idx [T][k] the ids it belongs to.  An id that occurs
+ *     twice in a token counts twice, ids outside [0,E) are ignored.  Nothing is divided by a gate: where it is 0, so is its part.
+ *   - the balance loss's part, where coef is given: coef [S][E] fp32 as grouter_balance left it for the same scores, gating,
+ *     token_mask, seq_offsets and S.  Tokens in no sequence have none.
+ * At least one of the two is given.  Without coef, seq_offsets is not read; without dlog_gate, topk_idx and k are not.
+ * Padding tokens get zeros.  Everything is computed in fp32 and rounded once.
+ */
+int grouter_route_bwd(const void* scores, int score_dtype, int64_t score_ld, int64_t T, int E, int gating,
+                      const uint8_t* token_mask, const void* topk_idx, int idx_dtype, int k, const float* dlog_gate,
+                      const int64_t* seq_offsets, int64_t S, const float* coef, void* dscores, int dscore_dtype,
+                      int64_t dscore_ld, void* stream);
+
+/* ---- balance loss and per-expert counts (the auxiliary loss of expert tuning, Sec. 3.2.3, per sequence) --
+ * With p_t the probabilities of token t over all experts (softmax of its scores; for the sigmoid gatings the sigmoids
+ * divided by their sum), for every sequence s of n valid tokens
+ *   f_e = counts[s][e] / (k n),  prob[s][e] = P_e = mean of p_te,  loss = alpha * sum_s E * sum_e f_e P_e .
+ *   seq_offsets [S+1] int64 ascending, in [0,T], or NULL with S = 1: one sequence of all T tokens.  Sequence s holds the
+ *            tokens [seq_offsets[s], seq_offsets[s+1]); it may be empty (its outputs are 0); tokens before the first or behind
+ *            the last are in none.
+ *   topk_idx [T][k]: the ids counted, once for every slot; ids outside [0,E) are ignored.
+ *   counts   [S][E] int32, prob [S][E] fp32, loss [1] fp32 (a sum over the sequences: alpha = a/S gives their mean)
+ *   coef     [S][E] fp32 = alpha * E * f_e / n, what grouter_route_bwd takes the loss's gradient from
+ *   ws       >= grouter_balance_bytes(T,E,S), 256-byte aligned; contents are dead after the call
+ * Bit-identical from run to run.
+ */
+size_t grouter_balance_bytes(int64_t T, int E, int64_t S);
+int grouter_balance(const void* scores, int score_dtype, int64_t score_ld, int64_t T, int E, int k, int gating,
+                    const uint8_t* token_mask, const void* topk_idx, int idx_dtype, const int64_t* seq_offsets, int64_t S,
+                    float alpha, int32_t* counts, float* prob, float* coef, float* loss, void* ws, size_t ws_bytes,
+                    void* stream);
+
+/* ---- gradient by the gates ------------------------------------------------------------------------------
+ * Row p of the layer's down product is O[p] = r f(x), r the gate of its slot, and y[t] the sum of a token's rows, so the
+ * gradient of L = <y, dY> by log r is <dY[t], O[p]>:  dlog_gate[t][j] = <dY[t][:], in[src_to_row[t*k+j]][:]> in fp32.
+ *   grouter_gate_bwd      in [N][d] bf16 rows in expert-sorted order, dY [T][d] bf16, dlog_gate [T][k] fp32
+ *   grouter_moe_gate_bwd  the same on the rows O that grouter_moe_fwd kept in ctx_ws
+ */
+int grouter_gate_bwd(const void* plan_ws, int64_t T, int k, int E, int d, const void* dY, const void* in,
+                     float* dlog_gate, void* stream);
+int grouter_moe_gate_bwd(const void* plan_ws, int64_t T, int k, int E, int d, int f, const void* dY, const void* ctx_ws,
+                         size_t ctx_ws_bytes, float* dlog_gate, void* stream);
+
+/* ---- AdamW over many tensors at once ----------------------------------------------------------------------
+ * With g = grad * grad_scale:  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   w = w - lr * weight_decay * w - lr/(1 - beta1^t) * m / (sqrt(v/(1 - beta2^t)) + eps),  all in fp32.
+ * Every tensor of a call has the same types:
+ *   param_kind  FP32: param fp32 is w.  MASTER: w is master (fp32), param (bf16) receives it rounded to nearest.
+ *               BF16: param (bf16) is w and is rounded up or down with the probability of the remainder (a step is often
+ *               less than half a unit of bf16, and rounding to nearest would lose it every time).
+ *   grad_dtype  GROUTER_FP32 or GROUTER_BF16
+ *   state_bits  32: m, v are fp32.  8: m holds m and v holds sqrt(v) as e4m3 numbers (1 byte), each 32 neighbours under one
+ *               power of two 2^(x - 127) with x in m_exp / v_exp [ceil(n/32)] uint8 (255: the block is NaN; it is so from the
+ *               first infinity or NaN on).  Rounded up or down with the probability of the remainder; a root above 0 never
+ *               becomes 0.  All zero bytes are a state of zeros.
+ * A tensor of n = 0 elements is skipped (its pointers may be NULL).  param, master, grad, m and v are 16-byte aligned.
+ * No tensor may overlap another one of the call.  The list is read during the call only.
+ * Random bits are a function of the seed and the element's place in the list (tensors one after the other, each rounded up
+ * to a multiple of 32): the same call gives the same result, and every step should bring another seed.
+ *   hyper / hyper_dev  exactly one is given: the host's, taken by value, or one in device memory, read when the step runs (a
+ *               captured step replays with what the buffer then holds).
+ *   grad_scale_dev     NULL, or one fp32 on the device that multiplies grad_scale (a clipping coefficient, 1/loss scale)
+ */
+enum { GROUTER_ADAMW_FP32 = 0, GROUTER_ADAMW_MASTER = 1, GROUTER_ADAMW_BF16 = 2 };
+typedef struct {
+    void* param;
+    float* master;
+    const void* grad;
+    void* m;
+    void* v;
+    uint8_t* m_exp;
+    uint8_t* v_exp;
+    int64_t n;
+} grouter_adamw_tensor;
+typedef struct {
+    float beta1, one_minus_beta1, beta2, one_minus_beta2;
+    float inv_root_correction; /* 1 / sqrt(1 - beta2^t) */
+    float eps;
+    float step_size;           /* lr / (1 - beta1^t) */
+    float decay;               /* lr * weight_decay */
+    float grad_scale;
+    uint32_t seed;
+    uint32_t reserved[2];
+} grouter_adamw_hyper;
+/* Fills `out` (host) for step t = 1, 2, ...: 0 <= beta1, beta2 < 1, eps > 0, finite lr, weight_decay and grad_scale. */
+int grouter_adamw_hyper_set(double lr, double beta1, double beta2, double eps, double weight_decay, int64_t step,
+                            double grad_scale, uint32_t seed, grouter_adamw_hyper* out);
+int grouter_adamw(const grouter_adamw_tensor* tensors, int count, int param_kind, int grad_dtype, int state_bits,
+                  const grouter_adamw_hyper* hyper, const grouter_adamw_hyper* hyper_dev, const float* grad_scale_dev,
+                  void* stream);
+
 /* ---- per-kernel timing (HIP events on the caller's stream) ----------------------------------------
  * While enabled, every phase (one kernel, or the few kernels of the plan build) is bracketed by events on
  * the stream it is launched on; consecutive phases inside one call share the event between them.  grouter_timing_read waits for those events and accumulates elapsed milliseconds and
@@ -245,7 +368,12 @@ enum {
     GROUTER_PH_COACT = 13,
     GROUTER_PH_FOLD = 14,      /* greedy grouping, folded weights */
     GROUTER_PH_SAMPLE_STATS = 15, /* grouter_sample_stats: affinity and placement in one pass */
-    GROUTER_PH_COUNT = 16
+    GROUTER_PH_ROUTE = 16,
+    GROUTER_PH_ROUTE_BWD = 17,
+    GROUTER_PH_BALANCE = 18,
+    GROUTER_PH_GATE_BWD = 19,
+    GROUTER_PH_ADAMW = 20,
+    GROUTER_PH_COUNT = 21
 };
 int grouter_timing_enable(int on);
 int grouter_timing_read(double* ms /*[GROUTER_PH_COUNT]*/, int64_t* launches /*[GROUTER_PH_COUNT]*/);

@@ -16,7 +16,10 @@ _lib = None
 OK, ERR_INVALID_ARG, ERR_WORKSPACE_TOO_SMALL, ERR_INDEX_OUT_OF_RANGE, ERR_HIP = 0, -1, -2, -3, -4
 IDX_INT32, IDX_UINT8 = 0, 1
 PHASES = ("plan", "permute", "gateup", "down", "combine", "dO", "dH", "dW2", "dW13", "dXp", "dX_reduce", "affinity",
-          "placement", "coactivation", "fold", "sample_stats")
+          "placement", "coactivation", "fold", "sample_stats", "route", "route_bwd", "balance", "gate_bwd", "adamw")
+FP32, BF16, FP16 = 0, 1, 2
+GATE_SOFTMAX_SELECTED, GATE_SOFTMAX_ALL, GATE_SIGMOID, GATE_SIGMOID_NORMALISED = 0, 1, 2, 3
+ADAMW_FP32, ADAMW_MASTER, ADAMW_BF16 = 0, 1, 2
 
 EXPORTS = (
     "grouter_strerror", "grouter_last_hip_error", "grouter_plan_bytes", "grouter_ctx_bytes",
@@ -25,6 +28,8 @@ EXPORTS = (
     "grouter_timing_read", "grouter_phase_name", "grouter_fwd_only_bytes", "grouter_moe_fwd_only", "grouter_affinity", "grouter_sample_placement",
     "grouter_coactivation", "grouter_fold_groups", "grouter_fold_weights", "grouter_static_ws_bytes",
     "grouter_moe_fwd_only_static", "grouter_sample_stats", "grouter_plan_set_gates", "grouter_mfma_probe",
+    "grouter_route", "grouter_route_bwd", "grouter_balance_bytes", "grouter_balance", "grouter_gate_bwd", "grouter_moe_gate_bwd",
+    "grouter_adamw_hyper_set", "grouter_adamw",
 )
 
 
@@ -35,6 +40,23 @@ class GrouterError(RuntimeError):
         if code == ERR_HIP:
             msg += f" (hipError_t {lib().grouter_last_hip_error()})"
         super().__init__(f"{where}: {msg}")
+
+
+class AdamWHyper(ctypes.Structure):
+    """One step's numbers (grouter_adamw_hyper), made by grouter_adamw_hyper."""
+
+    _fields_ = [(n, ctypes.c_float) for n in ("beta1", "one_minus_beta1", "beta2", "one_minus_beta2", "inv_root_correction", "eps",
+                                              "step_size", "decay", "grad_scale")] + [("seed", ctypes.c_uint32), ("reserved", ctypes.c_uint32 * 2)]
+
+    def tensor(self):
+        """The same as a uint8 CPU tensor of 48 bytes, to be copied into the device buffer of a captured step."""
+        import torch
+
+        return torch.frombuffer(bytearray(bytes(self)), dtype=torch.uint8)
+
+
+class _AdamWTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "master", "grad", "m", "v", "m_exp", "v_exp")] + [("n", ctypes.c_int64)]
 
 
 def lib():
@@ -84,6 +106,19 @@ def lib():
         L.grouter_fold_groups.argtypes = [vp, i32, i32, vp, vp]
         L.grouter_mfma_probe.argtypes = [i32, i32, i32, vp, sz, vp]
         L.grouter_fold_weights.argtypes = [vp, vp, i32, i32, i32, vp, vp]
+        f32, f64, u32 = ctypes.c_float, ctypes.c_double, ctypes.c_uint32
+        L.grouter_route.argtypes = [vp, i32, i64, i64, i32, i32, i32, vp, vp, i32, vp, vp]
+        L.grouter_route_bwd.argtypes = [vp, i32, i64, i64, i32, i32, vp, vp, i32, i32, vp, vp, i64, vp, vp, i32, i64, vp]
+        L.grouter_balance_bytes.argtypes = [i64, i32, i64]
+        L.grouter_balance_bytes.restype = sz
+        L.grouter_balance.argtypes = [vp, i32, i64, i64, i32, i32, i32, vp, vp, i32, vp, i64, f32, vp, vp, vp, vp, vp, sz, vp]
+        L.grouter_gate_bwd.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp, vp]
+        L.grouter_moe_gate_bwd.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, sz, vp, vp]
+        L.grouter_adamw_hyper_set.argtypes = [f64, f64, f64, f64, f64, i64, f64, u32, ctypes.POINTER(AdamWHyper)]
+        L.grouter_adamw.argtypes = [ctypes.POINTER(_AdamWTensor), i32, i32, i32, i32, ctypes.POINTER(AdamWHyper), vp, vp, vp]
+        for name in ("grouter_route", "grouter_route_bwd", "grouter_balance", "grouter_gate_bwd", "grouter_moe_gate_bwd",
+                     "grouter_adamw_hyper_set", "grouter_adamw"):
+            getattr(L, name).restype = i32
         for name in ("grouter_plan_build", "grouter_plan_views", "grouter_plan_status", "grouter_permute",
                      "grouter_combine", "grouter_moe_fwd", "grouter_moe_bwd", "grouter_timing_enable",
                      "grouter_timing_read", "grouter_affinity", "grouter_sample_placement", "grouter_coactivation",
@@ -389,6 +424,202 @@ def grouter_fold_weights(W_s, group_of, E_T, out, stream=None):
         raise ValueError("shape mismatch")
     _check(lib().grouter_fold_weights(_p(W_s), _p(group_of), d, E_S, E_T, _p(out), _stream(stream)),
            "grouter_fold_weights")
+
+
+def _float_dtype(t, name, allowed=(FP32, BF16, FP16)):
+    import torch
+
+    dt = {torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16}.get(t.dtype)
+    if dt not in allowed:
+        raise ValueError(f"{name} has an unsupported dtype ({t.dtype})")
+    return dt
+
+
+def _matrix(t, name):
+    """A GPU matrix whose rows are contiguous; its row stride may exceed its width."""
+    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{name} must be a GPU matrix with contiguous rows")
+    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+
+def _mask(token_mask, T):
+    import torch
+
+    if token_mask is None:
+        return None
+    _dev(token_mask, "token_mask")
+    if token_mask.dtype not in (torch.uint8, torch.bool) or token_mask.numel() != T:
+        raise ValueError("token_mask must be uint8 or bool [T]")
+    return token_mask.data_ptr()
+
+
+def _sequences(seq_offsets):
+    import torch
+
+    if seq_offsets is None:
+        return None, 1
+    _dev(seq_offsets, "seq_offsets", torch.int64)
+    if seq_offsets.dim() != 1 or seq_offsets.numel() < 2:
+        raise ValueError("seq_offsets must be int64 [S+1]")
+    return seq_offsets.data_ptr(), seq_offsets.numel() - 1
+
+
+def grouter_route(scores, k, gating, topk_idx, gate_w, token_mask=None, stream=None):
+    """scores [T,E] fp32/bf16/fp16 (rows may be apart); topk_idx [T,k] int32/uint8 and gate_w [T,k] bf16 are written."""
+    import torch
+
+    ld = _matrix(scores, "scores")
+    T, E = scores.shape
+    _dev(topk_idx, "topk_idx")
+    _dev(gate_w, "gate_w", torch.bfloat16)
+    if topk_idx.shape != (T, k) or gate_w.shape != (T, k):
+        raise ValueError("shape mismatch")
+    _check(lib().grouter_route(_p(scores), _float_dtype(scores, "scores"), ld, T, E, k, gating, _mask(token_mask, T), _p(topk_idx),
+                               _idx_dtype(topk_idx), _p(gate_w), _stream(stream)), "grouter_route")
+
+
+def grouter_route_bwd(scores, gating, dscores, topk_idx=None, dlog_gate=None, token_mask=None, seq_offsets=None, coef=None, stream=None):
+    """dscores [T,E] = gradient out of dlog_gate fp32 [T,k] at topk_idx and/or of the balance loss whose coef fp32 [S,E] is given."""
+    import torch
+
+    ld, dld = _matrix(scores, "scores"), _matrix(dscores, "dscores")
+    T, E = scores.shape
+    off, S = _sequences(seq_offsets) if coef is not None else (None, 1)
+    k = it = 0
+    if dlog_gate is not None:
+        _dev(dlog_gate, "dlog_gate", torch.float32)
+        _dev(topk_idx, "topk_idx")
+        k, it = topk_idx.shape[1], _idx_dtype(topk_idx)
+        if topk_idx.shape != (T, k) or dlog_gate.shape != (T, k):
+            raise ValueError("shape mismatch")
+    if coef is not None and _dev(coef, "coef", torch.float32).shape != (S, E) or dscores.shape != (T, E):
+        raise ValueError("shape mismatch")
+    _check(lib().grouter_route_bwd(_p(scores), _float_dtype(scores, "scores"), ld, T, E, gating, _mask(token_mask, T),
+                                   _p(topk_idx) if k else None, it, k, _p(dlog_gate), off, S, _p(coef), _p(dscores),
+                                   _float_dtype(dscores, "dscores"), dld, _stream(stream)), "grouter_route_bwd")
+
+
+def grouter_balance_bytes(T, E, S) -> int:
+    return int(lib().grouter_balance_bytes(T, E, S))
+
+
+def grouter_balance(scores, gating, topk_idx, alpha, counts, prob, coef, loss, ws, token_mask=None, seq_offsets=None, stream=None):
+    """scores [T,E], topk_idx [T,k], seq_offsets int64 [S+1] or None (S = 1); written: counts int32, prob and coef fp32 [S,E], loss fp32 [1]."""
+    import torch
+
+    ld = _matrix(scores, "scores")
+    T, E = scores.shape
+    off, S = _sequences(seq_offsets)
+    _dev(topk_idx, "topk_idx")
+    _dev(counts, "counts", torch.int32)
+    for t, n in ((prob, "prob"), (coef, "coef"), (loss, "loss")):
+        _dev(t, n, torch.float32)
+    k = topk_idx.shape[1]
+    if topk_idx.shape != (T, k) or counts.shape != (S, E) or prob.shape != (S, E) or coef.shape != (S, E) or loss.numel() != 1:
+        raise ValueError("shape mismatch")
+    _check(lib().grouter_balance(_p(scores), _float_dtype(scores, "scores"), ld, T, E, k, gating, _mask(token_mask, T), _p(topk_idx),
+                                 _idx_dtype(topk_idx), off, S, alpha, _p(counts), _p(prob), _p(coef), _p(loss), _p(_dev(ws, "ws")),
+                                 ws.numel() * ws.element_size(), _stream(stream)), "grouter_balance")
+
+
+def grouter_gate_bwd(plan_ws, T, k, E, dY, inp, dlog_gate, stream=None):
+    """dlog_gate fp32 [T,k] from dY bf16 [T,d] and rows inp bf16 [T*k,d] in expert-sorted order."""
+    import torch
+
+    _dev(plan_ws, "plan_ws")
+    for t, n in ((dY, "dY"), (inp, "in")):
+        _dev(t, n, torch.bfloat16)
+    _dev(dlog_gate, "dlog_gate", torch.float32)
+    d = dY.shape[1]
+    if dY.shape != (T, d) or inp.shape != (T * k, d) or dlog_gate.shape != (T, k) or plan_ws.numel() < grouter_plan_bytes(T, k, E):
+        raise ValueError("shape mismatch")
+    _check(lib().grouter_gate_bwd(_p(plan_ws), T, k, E, d, _p(dY), _p(inp), _p(dlog_gate), _stream(stream)), "grouter_gate_bwd")
+
+
+def grouter_moe_gate_bwd(plan_ws, E, f, dY, ctx_ws, dlog_gate, stream=None):
+    """The same on the rows that grouter_moe_fwd kept in ctx_ws."""
+    import torch
+
+    _dev(plan_ws, "plan_ws")
+    _dev(dY, "dY", torch.bfloat16)
+    _dev(ctx_ws, "ctx_ws")
+    _dev(dlog_gate, "dlog_gate", torch.float32)
+    T, k = dlog_gate.shape
+    d = dY.shape[1]
+    if dY.shape != (T, d) or plan_ws.numel() < grouter_plan_bytes(T, k, E):
+        raise ValueError("shape mismatch")
+    _check(lib().grouter_moe_gate_bwd(_p(plan_ws), T, k, E, d, f, _p(dY), _p(ctx_ws), ctx_ws.numel(), _p(dlog_gate), _stream(stream)),
+           "grouter_moe_gate_bwd")
+
+
+def grouter_adamw_hyper(lr, beta1, beta2, eps, weight_decay, step, grad_scale=1.0, seed=0) -> AdamWHyper:
+    h = AdamWHyper()
+    _check(lib().grouter_adamw_hyper_set(lr, beta1, beta2, eps, weight_decay, step, grad_scale, seed & 0xffffffff, ctypes.byref(h)),
+           "grouter_adamw_hyper_set")
+    return h
+
+
+class AdamWTensors:
+    """The tensors of an optimizer step, looked over once: lists of parameters, gradients and moments of one type each.
+
+    param fp32, or bf16, alone or with fp32 `master` copies; grad fp32 or bf16; m and v fp32, or uint8 codes with uint8 exponents
+    m_exp and v_exp of ceil(n/32) elements.  The object holds the tensors; a gradient that moves needs a new one.
+    """
+
+    def __init__(self, param, grad, m, v, master=None, m_exp=None, v_exp=None):
+        import torch
+
+        param, grad, m, v = list(param), list(grad), list(m), list(v)
+        none = [None] * len(param)
+        master, m_exp, v_exp = (none if x is None else list(x) for x in (master, m_exp, v_exp))
+        self._held = (param, grad, m, v, master, m_exp, v_exp)
+        if any(len(x) != len(param) for x in self._held):
+            raise ValueError("lists of different lengths")
+        self.count, self.device = len(param), param[0].device if param else None
+        first = param[0] if param else None
+        if first is not None and first.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("param must be fp32 or bf16")
+        if master is not none and first is not None and first.dtype != torch.bfloat16:
+            raise ValueError("master copies belong to bf16 parameters")
+        self.kind = ADAMW_FP32 if first is None or first.dtype == torch.float32 else ADAMW_BF16 if master is none else ADAMW_MASTER
+        self.grad_dtype = _float_dtype(grad[0], "grad", (FP32, BF16)) if grad else FP32
+        self.bits = 8 if m and m[0].dtype == torch.uint8 else 32
+        if (self.bits == 8) != (m_exp is not none) or (self.bits == 8) != (v_exp is not none):
+            if first is not None:
+                raise ValueError("8-bit moments come with exponents, 32-bit ones without")
+        state = torch.uint8 if self.bits == 8 else torch.float32
+        self._array = (_AdamWTensor * max(1, self.count))()
+        spans = []
+        for i, (p, g, a, b, w, ea, eb) in enumerate(zip(*self._held)):
+            n = p.numel()
+            for t, name, dtype, size in ((p, "param", first.dtype, n), (g, "grad", grad[0].dtype, n), (a, "m", state, n), (b, "v", state, n),
+                                         (w, "master", torch.float32, n), (ea, "m_exp", torch.uint8, -(-n // 32)),
+                                         (eb, "v_exp", torch.uint8, -(-n // 32))):
+                if t is None:
+                    continue
+                if _dev(t, name, dtype).numel() != size or t.device != self.device:
+                    raise ValueError(f"{name} {i}: wrong size or device")
+                if size and name not in ("m_exp", "v_exp") and t.data_ptr() % 16:
+                    raise ValueError(f"{name} {i} must be aligned to 16 bytes")
+                spans.append((t.data_ptr(), t.data_ptr() + size * t.element_size()))
+            self._array[i] = _AdamWTensor(*(_p(t) for t in (p, w, g, a, b, ea, eb)), n)
+        spans.sort()
+        if any(y[0] < x[1] for x, y in zip(spans, spans[1:]) if x[0] != x[1] and y[0] != y[1]):
+            raise ValueError("tensors overlap")
+
+
+def grouter_adamw(tensors, hyper, grad_scale=None, stream=None):
+    """One step over an AdamWTensors; hyper an AdamWHyper, or a GPU uint8 tensor holding one; grad_scale fp32 [1] on the GPU or None."""
+    import torch
+
+    host = isinstance(hyper, AdamWHyper)
+    if not host and _dev(hyper, "hyper", torch.uint8).numel() < ctypes.sizeof(AdamWHyper):
+        raise ValueError("hyper must hold 48 bytes")
+    if grad_scale is not None and _dev(grad_scale, "grad_scale", torch.float32).numel() != 1:
+        raise ValueError("grad_scale must have one element")
+    _check(lib().grouter_adamw(tensors._array, tensors.count, tensors.kind, tensors.grad_dtype, tensors.bits,
+                               ctypes.byref(hyper) if host else None, None if host else _p(hyper), _p(grad_scale), _stream(stream)),
+           "grouter_adamw")
 
 
 def grouter_timing_enable(on: bool):

@@ -1,0 +1,257 @@
+// One AdamW step over many tensors: with g the scaled gradient,
+//   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  w = w - (lr wd w + lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)).
+//
+// A pass over memory and nothing else: 22 to 30 bytes per element with 32-bit moments, 10 to 18 with 8-bit ones.  A launch takes the
+// addresses of up to kAdamwPerLaunch tensors in its arguments (nothing to copy to the device first, and a graph holds them by value);
+// its workgroups are dealt to the tensors by size.
+//
+// 8-bit moments.  m and r = sqrt(v) are e4m3 numbers (4 exponent bits, 3 mantissa bits, largest 448) times a power of two per 32
+// neighbours, the smallest under which the largest is at most 448.  A root spans in 8 bits what v would need 16 binades more for.
+// Both are rounded up or down with the probability of the remainder: v changes by a thousandth per step at b2 = 0.999, which rounding to
+// nearest would throw away every time.  A root above zero never becomes zero (a step divided by eps alone would follow), a block with an
+// infinity or NaN becomes NaN as a whole.  The random bits are a function of the element's number and the seed.
+//
+// The moments are computed with separately rounded products and sums (no fused multiply-add), so that their codes follow from the
+// formulas alone.
+#include "lanes.hpp"
+
+#pragma clang fp contract(off)
+
+namespace grouter {
+
+namespace {
+
+constexpr int kThreads = 256, kEach = 8;              // elements of a thread: 16 bytes of bf16, a quarter of a block of moments
+constexpr int kBlock = 32;                            // elements under one exponent
+constexpr int kPasses = 4;
+constexpr int64_t kPerGroup = kThreads * kEach * kPasses;
+
+enum ParamKind { kFp32Param = 0, kMasterParam = 1, kBf16Param = 2 };
+
+struct Batch {
+    AdamwTensor tensor[kAdamwPerLaunch];
+    uint32_t first_group[kAdamwPerLaunch + 1];        // workgroups before each tensor
+    uint64_t first_place[kAdamwPerLaunch];            // elements before each tensor, every tensor rounded up to whole blocks
+    int count;
+    AdamwHyper hyper;
+    const AdamwHyper* hyper_device;
+    const float* grad_scale;
+};
+static_assert(sizeof(Batch) <= 4000, "a launch's arguments are limited to 4 KB");
+
+__device__ __forceinline__ uint32_t noise_of(uint64_t place, uint32_t seed) {
+    uint32_t h = (uint32_t)place + (uint32_t)(place >> 32) * 0x632BE5ABu + seed * 0x9E3779B1u;
+    h ^= h >> 16;
+    h *= 0xA3D95FA9u;
+    h ^= h >> 15;
+    h *= 0x7B1D4E65u;
+    return h ^ (h >> 16);
+}
+
+// sqrt(v) to 1 unit; the hardware's takes what is below 2^-126 for 0
+__device__ __forceinline__ float root_of(float v) {
+    const bool small = v < 0x1p-96f;
+    return __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v) * (small ? 0x1p-32f : 1.f);
+}
+__device__ __forceinline__ float power_of_two(int biased) {   // 2^(biased - 127); 255 is NaN
+    return __uint_as_float(biased == 255 ? 0x7fc00000u : biased == 0 ? 0x00400000u : (uint32_t)biased << 23);
+}
+// e4m3 code of x >= 0 times 2^(127 - exp); up: 20 random bits
+__device__ __forceinline__ uint32_t code_of(float x, int exp, uint32_t up) {
+    const float y = x * power_of_two(254 - exp);
+    const uint32_t normal = ((__float_as_uint(y) + up) >> 20) - 960u;
+    const uint32_t small = (uint32_t)(y * 512.f + (float)up * 0x1p-20f);
+    return exp == 255 ? 127u : min(y < 0x1p-6f ? small : normal, 126u);
+}
+__device__ __forceinline__ void decode4(uint32_t codes, float scale, float* out) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+    out[0] = a.x * scale;
+    out[1] = a.y * scale;
+    out[2] = b.x * scale;
+    out[3] = b.y * scale;
+}
+
+// kEach elements from p on, n of them there, the others 0
+template <class Type>
+__device__ __forceinline__ void fetch(const void* p, int64_t at, int n, float* out) {
+    const auto* q = (const typename Type::stored*)p + at;
+    if (n == kEach) {
+        typename Type::stored raw[kEach];
+        __builtin_memcpy(raw, __builtin_assume_aligned(q, 16), sizeof(raw));
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) out[i] = Type::widen(raw[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) out[i] = i < n ? Type::widen(q[i]) : 0.f;
+    }
+}
+template <class T>
+__device__ __forceinline__ void put(T* p, int64_t at, int n, const T* v) {
+    if (n == kEach) {
+        __builtin_memcpy(__builtin_assume_aligned(p + at, sizeof(T) == 1 ? 8 : 16), v, sizeof(T) * kEach);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (i < n) p[at + i] = v[i];
+    }
+}
+
+template <int KIND, class Grad, bool EIGHT>
+__global__ __launch_bounds__(kThreads) void k_adamw(const Batch batch) {
+    int i = 0;
+    for (int step = 32; step > 0; step /= 2)
+        if (i + step < batch.count && batch.first_group[i + step] <= blockIdx.x) i += step;
+    const AdamwTensor t = batch.tensor[i];
+    const AdamwHyper h = batch.hyper_device ? *batch.hyper_device : batch.hyper;
+    const float scale = batch.grad_scale ? h.grad_scale * *batch.grad_scale : h.grad_scale;
+    const int64_t begin = (int64_t)(blockIdx.x - batch.first_group[i]) * kPerGroup;
+#pragma unroll
+    for (int pass = 0; pass < kPasses; ++pass) {
+        const int64_t at = begin + ((int64_t)pass * kThreads + threadIdx.x) * kEach;
+        const int n = (int)max((int64_t)0, min((int64_t)kEach, t.n - at));
+        if (__ballot(n > 0) == 0) return;
+        float g[kEach], m[kEach], v[kEach], w[kEach];
+        fetch<Grad>(t.grad, n ? at : 0, n, g);
+        if (KIND == kBf16Param) fetch<Bf16>(t.param, n ? at : 0, n, w);
+        else fetch<Fp32>(KIND == kMasterParam ? t.master : t.param, n ? at : 0, n, w);
+        if (EIGHT) {
+            uint32_t cm[2] = {0, 0}, cv[2] = {0, 0};
+            const auto* qm = (const uint8_t*)t.m + at;
+            const auto* qv = (const uint8_t*)t.v + at;
+            if (n == kEach) {
+                __builtin_memcpy(cm, __builtin_assume_aligned(qm, 8), 8);
+                __builtin_memcpy(cv, __builtin_assume_aligned(qv, 8), 8);
+            } else {
+                for (int j = 0; j < n; ++j) {
+                    cm[j / 4] |= (uint32_t)qm[j] << (8 * (j & 3));
+                    cv[j / 4] |= (uint32_t)qv[j] << (8 * (j & 3));
+                }
+            }
+            const float sm = power_of_two(n ? t.m_exp[at / kBlock] : 0), sv = power_of_two(n ? t.v_exp[at / kBlock] : 0);
+            decode4(cm[0], sm, m);
+            decode4(cm[1], sm, m + 4);
+            decode4(cv[0], sv, v);
+            decode4(cv[1], sv, v + 4);
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) v[j] = v[j] * v[j];
+        } else {
+            fetch<Fp32>(t.m, n ? at : 0, n, m);
+            fetch<Fp32>(t.v, n ? at : 0, n, v);
+        }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const float s = g[j] * scale;
+            m[j] = m[j] * h.beta1 + s * h.one_minus_beta1;
+            v[j] = v[j] * h.beta2 + s * s * h.one_minus_beta2;
+            w[j] = w[j] - (w[j] * h.decay + m[j] * __builtin_amdgcn_rcpf(root_of(v[j]) * h.inv_root_correction + h.eps) * h.step_size);
+        }
+        uint32_t noise[kEach];
+        if (EIGHT || KIND == kBf16Param) {
+            const uint64_t place = batch.first_place[i] + at;
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) noise[j] = noise_of(place + j, h.seed);
+        }
+        if (KIND == kFp32Param) put((float*)t.param, at, n, w);
+        if (KIND == kMasterParam) put(t.master, at, n, w);
+        if (KIND != kFp32Param) {
+            uint16_t b[kEach];
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                b[j] = Bf16::narrow(w[j]);
+                if (KIND == kBf16Param) {   // a step is often less than half a unit of bf16: up or down with the probability of the remainder
+                    const uint32_t u = __float_as_uint(w[j]);
+                    b[j] = (u & 0x7fffffffu) < 0x7f800000u ? (uint16_t)((u + (noise[j] >> 16)) >> 16) : b[j];
+                }
+            }
+            put((uint16_t*)t.param, at, n, b);
+        }
+        if (!EIGHT) {
+            put((float*)t.m, at, n, m);
+            put((float*)t.v, at, n, v);
+        } else {
+            uint32_t pm = 0, pv = 0;
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                pm = max(pm, __float_as_uint(m[j]) & 0x7fffffffu);
+                pv = max(pv, __float_as_uint(v[j]));
+            }
+            pm = group_max<kBlock / kEach>(pm);
+            pv = group_max<kBlock / kEach>(pv);
+            // the least power of two under which the largest is at most 448 = 1.75 * 2^8; for the root of v, 1.75^2 = 3.0625 per 4^k
+            const int em = pm >= 0x7f800000u ? 255 : max((int)((pm + 0x1fffffu) >> 23) - 8, 0);
+            // (numbers below 2^-126 have no leading bit to go by: 56 fits them all)
+            const int ev = pv >= 0x7f800000u ? 255 : pv - 1u < 0x7fffffu ? 56 : (((int)pv - (127 << 23) + 0x3bffff) >> 24) + 119;
+            uint8_t cm[kEach], cv[kEach];
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                cm[j] = (uint8_t)(code_of(fabsf(m[j]), em, noise[j] >> 12) | (__float_as_uint(m[j]) >> 31 << 7));
+                const uint32_t c = code_of(root_of(v[j]), ev, (noise[j] & 0xfffu) << 8 | 128u);
+                cv[j] = (uint8_t)(v[j] > 0.f ? max(c, 1u) : c);
+            }
+            put((uint8_t*)t.m, at, n, cm);
+            put((uint8_t*)t.v, at, n, cv);
+            if (n > 0 && at % kBlock == 0) {
+                t.m_exp[at / kBlock] = (uint8_t)em;
+                t.v_exp[at / kBlock] = (uint8_t)ev;
+            }
+        }
+    }
+}
+
+template <int KIND, class Grad, bool EIGHT>
+hipError_t launch(const Batch& b, unsigned groups, hipStream_t s) {
+    hipLaunchKernelGGL((k_adamw<KIND, Grad, EIGHT>), dim3(groups), dim3(kThreads), 0, s, b);
+    return hipGetLastError();
+}
+
+hipError_t launch_batch(const Batch& b, unsigned groups, int kind, int grad_dtype, int bits, hipStream_t s) {
+    if (groups == 0) return hipSuccess;
+#define GROUTER_CASE(KIND)                                                                                      \
+    if (kind == KIND) {                                                                                         \
+        if (grad_dtype == 0) return bits == 8 ? launch<KIND, Fp32, true>(b, groups, s) : launch<KIND, Fp32, false>(b, groups, s); \
+        return bits == 8 ? launch<KIND, Bf16, true>(b, groups, s) : launch<KIND, Bf16, false>(b, groups, s);   \
+    }
+    GROUTER_CASE(kFp32Param)
+    GROUTER_CASE(kMasterParam)
+    GROUTER_CASE(kBf16Param)
+#undef GROUTER_CASE
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_adamw(const AdamwTensor* tensors, int count, int param_kind, int grad_dtype, int state_bits, const AdamwHyper* host,
+                        const AdamwHyper* device, const float* grad_scale, hipStream_t s) {
+    Batch b{};
+    if (host) b.hyper = *host;
+    b.hyper_device = device;
+    b.grad_scale = grad_scale;
+    uint64_t place = 0;
+    uint64_t groups = 0;
+    auto flush = [&]() {
+        b.first_group[b.count] = (uint32_t)groups;
+        const hipError_t e = launch_batch(b, (unsigned)groups, param_kind, grad_dtype, state_bits, s);
+        b.count = 0;
+        groups = 0;
+        return e;
+    };
+    for (int i = 0; i < count; ++i) {
+        const uint64_t need = ((uint64_t)tensors[i].n + kPerGroup - 1) / kPerGroup;
+        if (tensors[i].n > 0) {
+            if (b.count == kAdamwPerLaunch || groups + need > 0x7fffffffu) {
+                const hipError_t e = flush();
+                if (e != hipSuccess) return e;
+            }
+            b.tensor[b.count] = tensors[i];
+            b.first_group[b.count] = (uint32_t)groups;
+            b.first_place[b.count] = place;
+            ++b.count;
+            groups += need;
+        }
+        place += ((uint64_t)tensors[i].n + kBlock - 1) / kBlock * kBlock;
+    }
+    return flush();
+}
+
+}  // namespace grouter

@@ -1,6 +1,7 @@
 // C ABI of the grouter library (see include/grouter.h): argument checks, workspace carving, launch order.
 #include "../../include/grouter.h"
 
+#include <cmath>
 #include <mutex>
 #include <vector>
 
@@ -501,6 +502,141 @@ int grouter_fold_weights(const float* W_s, const int32_t* group_of, int d, int E
     return e == hipSuccess ? GROUTER_OK : fail_hip(e);
 }
 
+// ---- the router and what trains it -------------------------------------------------------------------------
+namespace {
+constexpr int64_t kMaxSequences = 1 << 24;
+
+bool type_ok(int dtype) { return dtype == GROUTER_FP32 || dtype == GROUTER_BF16 || dtype == GROUTER_FP16; }
+size_t type_bytes(int dtype) { return dtype == GROUTER_FP32 ? 4 : 2; }
+bool aligned_to(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+bool ids_ok(const void* ids, int idx_dtype, int E) {
+    if (idx_dtype == GROUTER_IDX_INT32) return ids && aligned_to(ids, 4);
+    return ids && idx_dtype == GROUTER_IDX_UINT8 && E <= 256;
+}
+// a matrix of T rows of E elements, ld apart, whose byte offsets fit 63 bits
+bool matrix_ok(const void* p, int dtype, int64_t ld, int64_t T, int E) {
+    return p && type_ok(dtype) && aligned_to(p, type_bytes(dtype)) && T > 0 && T <= 0x7fffffff && E > 0 && E <= kMaxExperts && ld >= E &&
+           ld <= (1ll << 31);
+}
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+}  // namespace
+
+int grouter_route(const void* scores, int score_dtype, int64_t score_ld, int64_t T, int E, int k, int gating,
+                  const uint8_t* token_mask, void* topk_idx, int idx_dtype, void* gate_w, void* stream) {
+    if (!matrix_ok(scores, score_dtype, score_ld, T, E) || !dims_ok(T, k, E) || !ids_ok(topk_idx, idx_dtype, E)) return GROUTER_ERR_INVALID_ARG;
+    if (!gate_w || !aligned_to(gate_w, 2) || gating < GROUTER_GATE_SOFTMAX_SELECTED || gating > GROUTER_GATE_SIGMOID_NORMALISED)
+        return GROUTER_ERR_INVALID_ARG;
+    hipStream_t s = (hipStream_t)stream;
+    PhaseTimer tm(GROUTER_PH_ROUTE, s);
+    const hipError_t e = launch_route(scores, score_dtype, score_ld, T, E, k, gating, token_mask, topk_idx, idx_dtype, (uint16_t*)gate_w, s);
+    return e == hipSuccess ? GROUTER_OK : fail_hip(e);
+}
+
+int grouter_route_bwd(const void* scores, int score_dtype, int64_t score_ld, int64_t T, int E, int gating,
+                      const uint8_t* token_mask, const void* topk_idx, int idx_dtype, int k, const float* dlog_gate,
+                      const int64_t* seq_offsets, int64_t S, const float* coef, void* dscores, int dscore_dtype,
+                      int64_t dscore_ld, void* stream) {
+    if (!matrix_ok(scores, score_dtype, score_ld, T, E) || !matrix_ok(dscores, dscore_dtype, dscore_ld, T, E)) return GROUTER_ERR_INVALID_ARG;
+    if (gating < GROUTER_GATE_SOFTMAX_SELECTED || gating > GROUTER_GATE_SIGMOID_NORMALISED || (!dlog_gate && !coef)) return GROUTER_ERR_INVALID_ARG;
+    if (dlog_gate && (!dims_ok(T, k, E) || !ids_ok(topk_idx, idx_dtype, E) || !aligned_to(dlog_gate, 4))) return GROUTER_ERR_INVALID_ARG;
+    if (coef && (S < 1 || S > kMaxSequences || (!seq_offsets && S != 1) || !aligned_to(coef, 4) || !aligned_to(seq_offsets, 8)))
+        return GROUTER_ERR_INVALID_ARG;
+    const size_t span = ((size_t)(T - 1) * score_ld + E) * type_bytes(score_dtype), out_span = ((size_t)(T - 1) * dscore_ld + E) * type_bytes(dscore_dtype);
+    if (overlap(scores, span, dscores, out_span)) return GROUTER_ERR_INVALID_ARG;
+    hipStream_t s = (hipStream_t)stream;
+    PhaseTimer tm(GROUTER_PH_ROUTE_BWD, s);
+    const hipError_t e = launch_route_bwd(scores, score_dtype, score_ld, T, E, gating, token_mask, topk_idx, idx_dtype, k, dlog_gate,
+                                          coef ? seq_offsets : nullptr, S, coef, dscores, dscore_dtype, dscore_ld, s);
+    return e == hipSuccess ? GROUTER_OK : fail_hip(e);
+}
+
+size_t grouter_balance_bytes(int64_t T, int E, int64_t S) {
+    if (T <= 0 || T > 0x7fffffff || E <= 0 || E > kMaxExperts || S < 1 || S > kMaxSequences) return 0;
+    return balance_layout(T, E, S).total;
+}
+
+int grouter_balance(const void* scores, int score_dtype, int64_t score_ld, int64_t T, int E, int k, int gating,
+                    const uint8_t* token_mask, const void* topk_idx, int idx_dtype, const int64_t* seq_offsets, int64_t S,
+                    float alpha, int32_t* counts, float* prob, float* coef, float* loss, void* ws, size_t ws_bytes,
+                    void* stream) {
+    if (!matrix_ok(scores, score_dtype, score_ld, T, E) || !dims_ok(T, k, E) || !ids_ok(topk_idx, idx_dtype, E)) return GROUTER_ERR_INVALID_ARG;
+    if (gating < GROUTER_GATE_SOFTMAX_SELECTED || gating > GROUTER_GATE_SIGMOID_NORMALISED) return GROUTER_ERR_INVALID_ARG;
+    if (S < 1 || S > kMaxSequences || (!seq_offsets && S != 1) || !aligned_to(seq_offsets, 8)) return GROUTER_ERR_INVALID_ARG;
+    if (!counts || !prob || !coef || !loss || !aligned_to(counts, 4) || !aligned_to(prob, 4) || !aligned_to(coef, 4) || !aligned_to(loss, 4))
+        return GROUTER_ERR_INVALID_ARG;
+    if (!ws || !aligned256(ws)) return GROUTER_ERR_INVALID_ARG;
+    if (ws_bytes < balance_layout(T, E, S).total) return GROUTER_ERR_WORKSPACE_TOO_SMALL;
+    hipStream_t s = (hipStream_t)stream;
+    PhaseTimer tm(GROUTER_PH_BALANCE, s);
+    const hipError_t e = launch_balance(scores, score_dtype, score_ld, T, E, k, gating >= GROUTER_GATE_SIGMOID, token_mask, topk_idx, idx_dtype,
+                                        seq_offsets, S, alpha, counts, prob, coef, loss, ws, s);
+    return e == hipSuccess ? GROUTER_OK : fail_hip(e);
+}
+
+int grouter_gate_bwd(const void* plan_ws, int64_t T, int k, int E, int d, const void* dY, const void* in, float* dlog_gate, void* stream) {
+    if (!plan_ws || !dY || !in || !dlog_gate || !dims_ok(T, k, E) || d <= 0 || (d % 8)) return GROUTER_ERR_INVALID_ARG;
+    if (!aligned16(dY) || !aligned16(in) || !aligned_to(dlog_gate, 4)) return GROUTER_ERR_INVALID_ARG;
+    const PlanView P = make_plan_view(plan_ws, make_plan_layout(T, k, E));
+    hipStream_t s = (hipStream_t)stream;
+    PhaseTimer tm(GROUTER_PH_GATE_BWD, s);
+    const hipError_t e = launch_gate_bwd(P, d, (const bf16_t*)dY, (const bf16_t*)in, dlog_gate, s);
+    return e == hipSuccess ? GROUTER_OK : fail_hip(e);
+}
+
+int grouter_moe_gate_bwd(const void* plan_ws, int64_t T, int k, int E, int d, int f, const void* dY, const void* ctx_ws,
+                         size_t ctx_ws_bytes, float* dlog_gate, void* stream) {
+    if (!ctx_ws || !aligned256(ctx_ws) || !widths_ok(T, k, E, d, f)) return GROUTER_ERR_INVALID_ARG;
+    const CtxLayout C = ctx_layout(T, k, d, f);
+    if (ctx_ws_bytes < C.total) return GROUTER_ERR_WORKSPACE_TOO_SMALL;
+    return grouter_gate_bwd(plan_ws, T, k, E, d, dY, (const char*)ctx_ws + C.o, dlog_gate, stream);
+}
+
+int grouter_adamw_hyper_set(double lr, double beta1, double beta2, double eps, double weight_decay, int64_t step, double grad_scale,
+                            uint32_t seed, grouter_adamw_hyper* out) {
+    if (!out || step < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps > 0.0) || !std::isfinite(eps) ||
+        !std::isfinite(lr) || !std::isfinite(weight_decay) || !std::isfinite(grad_scale))
+        return GROUTER_ERR_INVALID_ARG;
+    *out = grouter_adamw_hyper{};
+    out->beta1 = (float)beta1;
+    out->one_minus_beta1 = (float)(1.0 - beta1);
+    out->beta2 = (float)beta2;
+    out->one_minus_beta2 = (float)(1.0 - beta2);
+    out->inv_root_correction = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
+    out->eps = (float)eps;
+    out->step_size = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
+    out->decay = (float)(lr * weight_decay);
+    out->grad_scale = (float)grad_scale;
+    out->seed = seed;
+    return GROUTER_OK;
+}
+
+static_assert(sizeof(grouter_adamw_tensor) == sizeof(AdamwTensor) && sizeof(grouter_adamw_hyper) == sizeof(AdamwHyper),
+              "the library's own structures have the header's layout");
+
+int grouter_adamw(const grouter_adamw_tensor* tensors, int count, int param_kind, int grad_dtype, int state_bits,
+                  const grouter_adamw_hyper* hyper, const grouter_adamw_hyper* hyper_dev, const float* grad_scale_dev, void* stream) {
+    if (count < 0 || (count > 0 && !tensors) || (hyper != nullptr) == (hyper_dev != nullptr)) return GROUTER_ERR_INVALID_ARG;
+    if (param_kind < GROUTER_ADAMW_FP32 || param_kind > GROUTER_ADAMW_BF16 || (grad_dtype != GROUTER_FP32 && grad_dtype != GROUTER_BF16) ||
+        (state_bits != 8 && state_bits != 32) || !aligned_to(hyper_dev, 4) || !aligned_to(grad_scale_dev, 4))
+        return GROUTER_ERR_INVALID_ARG;
+    for (int i = 0; i < count; ++i) {
+        const grouter_adamw_tensor& t = tensors[i];
+        if (t.n < 0 || t.n > (1ll << 40)) return GROUTER_ERR_INVALID_ARG;
+        if (t.n == 0) continue;
+        if (!t.param || !t.grad || !t.m || !t.v || (param_kind == GROUTER_ADAMW_MASTER) != (t.master != nullptr) ||
+            (state_bits == 8) != (t.m_exp != nullptr) || (state_bits == 8) != (t.v_exp != nullptr))
+            return GROUTER_ERR_INVALID_ARG;
+        if (!aligned16(t.param) || !aligned16(t.master) || !aligned16(t.grad) || !aligned16(t.m) || !aligned16(t.v)) return GROUTER_ERR_INVALID_ARG;
+    }
+    hipStream_t s = (hipStream_t)stream;
+    PhaseTimer tm(GROUTER_PH_ADAMW, s);
+    const hipError_t e = launch_adamw((const AdamwTensor*)tensors, count, param_kind, grad_dtype, state_bits, (const AdamwHyper*)hyper,
+                                      (const AdamwHyper*)hyper_dev, grad_scale_dev, s);
+    return e == hipSuccess ? GROUTER_OK : fail_hip(e);
+}
+
 int grouter_mfma_probe(int mode, int iters, int workgroups, float* out, size_t out_elems, void* stream) {
     if (!out || mode < 0 || mode > 7 || iters <= 0 || (iters & 3) || workgroups <= 0 || workgroups > (1 << 20))
         return GROUTER_ERR_INVALID_ARG;
@@ -549,7 +685,8 @@ int grouter_timing_read(double* ms, int64_t* launches) {
 const char* grouter_phase_name(int phase) {
     static const char* names[GROUTER_PH_COUNT] = {"plan", "permute", "gateup", "down", "combine", "dO",
                                                   "dH", "dW2", "dW13", "dXp", "dX_reduce", "affinity",
-                                                  "placement", "coactivation", "fold", "sample_stats"};
+                                                  "placement", "coactivation", "fold", "sample_stats", "route", "route_bwd",
+                                                  "balance", "gate_bwd", "adamw"};
     return (phase >= 0 && phase < GROUTER_PH_COUNT) ? names[phase] : "?";
 }
 

@@ -126,6 +126,41 @@ hipError_t launch_row_gates(const PlanView& P, const bf16_t* gate_w, float* row_
 hipError_t launch_permute(const PlanView& P, int d, const bf16_t* in, const bf16_t* gate_w, bf16_t* out, hipStream_t s);
 hipError_t launch_combine(const PlanView& P, int d, const bf16_t* in, const bf16_t* gate_w, bf16_t* out, hipStream_t s);
 
+// router and balance loss (router.hip); dtypes are GROUTER_FP32 ..., gating GROUTER_GATE_...
+struct BalanceLayout {
+    size_t done, loss, tokens, sum, count, total;
+    int64_t rows, chunks;   // the tokens are cut into `chunks` runs of `rows`
+};
+BalanceLayout balance_layout(int64_t T, int E, int64_t S);
+hipError_t launch_route(const void* scores, int dtype, int64_t ld, int64_t T, int E, int k, int gating, const uint8_t* token_mask, void* ids,
+                        int idx_dtype, uint16_t* gates, hipStream_t s);
+hipError_t launch_route_bwd(const void* scores, int dtype, int64_t ld, int64_t T, int E, int gating, const uint8_t* token_mask, const void* ids,
+                            int idx_dtype, int k, const float* dlog, const int64_t* off, int64_t S, const float* coef, void* out,
+                            int out_dtype, int64_t out_ld, hipStream_t s);
+hipError_t launch_balance(const void* scores, int dtype, int64_t ld, int64_t T, int E, int k, bool sigmoid, const uint8_t* token_mask, const void* ids,
+                          int idx_dtype, const int64_t* off, int64_t S, float alpha, int32_t* counts, float* prob, float* coef,
+                          float* loss, void* ws, hipStream_t s);
+hipError_t launch_gate_bwd(const PlanView& P, int d, const bf16_t* dY, const bf16_t* rows, float* dlog, hipStream_t s);
+
+// optimizer (adamw.hip)
+constexpr int kAdamwPerLaunch = 40;   // tensors that a launch takes in its arguments
+struct AdamwTensor {
+    void* param;
+    float* master;
+    const void* grad;
+    void* m;
+    void* v;
+    uint8_t* m_exp;
+    uint8_t* v_exp;
+    int64_t n;
+};
+struct AdamwHyper {
+    float beta1, one_minus_beta1, beta2, one_minus_beta2, inv_root_correction, eps, step_size, decay, grad_scale;
+    uint32_t seed, reserved[2];
+};
+hipError_t launch_adamw(const AdamwTensor* tensors, int count, int param_kind, int grad_dtype, int state_bits, const AdamwHyper* host,
+                        const AdamwHyper* device, const float* grad_scale, hipStream_t s);
+
 // Grouped GEMM phases.  Activation matrices are [N][d] or [N][f] in expert-sorted row order.  dSdG and dSdU are
 // the partial derivatives of S = silu(G) * U by G and by U, which the forward pass keeps for backward instead of G, U.
 hipError_t launch_gateup(const PlanView& P, int d, int f, const bf16_t* x, const float* row_gate, const bf16_t* W1,

@@ -8,7 +8,7 @@
 // lanes cover consecutive 16-byte pieces of one row, so every global access is a full contiguous row
 // segment.  The payload itself does not pass through LDS - rows are at least 16 bytes wide and already
 // contiguous, so staging them would only add latency.
-#include "common.hpp"
+#include "lanes.hpp"
 
 namespace grouter {
 
@@ -138,6 +138,34 @@ __global__ __launch_bounds__(256) void k_row_gates(const PlanDims plan, const in
     if (!plan.match()) return;
     const int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (p < N) row_gate[p] = __uint_as_float((uint32_t)gate_w[row_to_src[p]] << 16);
+}
+
+// dlog[i] = <dY[t], in[src_to_row[i]]>, i = t*k + j: the gradient by the log of a slot's gate, since the row is the gate times what
+// does not depend on it.  One wave per slot: the k rows of a token are read once each, dY's row comes from L1 for all but the first.
+__global__ __launch_bounds__(256) void k_gate_bwd(const PlanDims plan, const int32_t* __restrict__ src_to_row, int64_t N, int k, int chunks_per_row,
+                                                  const u32x4* __restrict__ dY, const u32x4* __restrict__ in, float* __restrict__ dlog) {
+    if (!plan.match()) return;
+    const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (i >= N) return;
+    const int lane = threadIdx.x & 63;
+    const u32x4* a = dY + (size_t)(i / k) * chunks_per_row;
+    const u32x4* b = in + (size_t)src_to_row[i] * chunks_per_row;
+    float acc = 0.f;
+    for (int c = lane; c < chunks_per_row; c += 64) {
+        const u32x4 u = a[c], v = __builtin_nontemporal_load(b + c);
+        acc += bf16_lo(u.x) * bf16_lo(v.x) + bf16_hi(u.x) * bf16_hi(v.x);
+        acc += bf16_lo(u.y) * bf16_lo(v.y) + bf16_hi(u.y) * bf16_hi(v.y);
+        acc += bf16_lo(u.z) * bf16_lo(v.z) + bf16_hi(u.z) * bf16_hi(v.z);
+        acc += bf16_lo(u.w) * bf16_lo(v.w) + bf16_hi(u.w) * bf16_hi(v.w);
+    }
+    acc = group_sum<64>(acc);
+    if (lane == 0) dlog[i] = acc;
+}
+
+hipError_t launch_gate_bwd(const PlanView& P, int d, const bf16_t* dY, const bf16_t* rows, float* dlog, hipStream_t s) {
+    hipLaunchKernelGGL(k_gate_bwd, dim3((unsigned)((P.N + 3) / 4)), dim3(256), 0, s, P.dims(), P.src_to_row, P.N, P.k, d / 8, (const u32x4*)dY,
+                       (const u32x4*)rows, dlog);
+    return hipGetLastError();
 }
 
 hipError_t launch_row_gates(const PlanView& P, const bf16_t* gate_w, float* row_gate, hipStream_t s) {
