@@ -128,7 +128,7 @@ hipError_t launch_combine(const PlanView& P, int d, const bf16_t* in, const bf16
 
 // router and balance loss (router.hip); dtypes are GROUTER_FP32 ..., gating GROUTER_GATE_...
 struct BalanceLayout {
-    size_t done, loss, tokens, sum, count, total;
+    size_t done, loss, tokens, cells, total;
     int64_t rows, chunks;   // the tokens are cut into `chunks` runs of `rows`
 };
 BalanceLayout balance_layout(int64_t T, int E, int64_t S);

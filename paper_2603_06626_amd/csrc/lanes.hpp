@@ -45,11 +45,13 @@ struct Fp32 {
 };
 struct Bf16 {
     typedef uint16_t stored;
+    static constexpr uint16_t kInf = 0x7f80;
     static __device__ __forceinline__ float widen(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
     static __device__ __forceinline__ uint16_t narrow(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }   // to nearest, ties to even
 };
 struct Fp16 {
     typedef uint16_t stored;
+    static constexpr uint16_t kInf = 0x7c00;
     static __device__ __forceinline__ float widen(uint16_t v) { return (float)__builtin_bit_cast(_Float16, v); }
     static __device__ __forceinline__ uint16_t narrow(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
 };

@@ -1,9 +1,10 @@
 // The router of an expert layer: scores -> expert ids and gate weights (Eq. 2, r = g(TopK(s, k))), the way back, and the balance loss
 // with per-expert counts.
 //
-// All three read a row of E scores per token.  A token belongs to a group of L neighbouring lanes, each of which holds V consecutive
-// scores (V = 8 up to 512 experts, 16 beyond), so a wave works on 64 / L tokens at a time, a row is read with whole 16-byte loads,
-// and every reduction over a row is one inside registers and log2(L) cross-lane moves.
+// All of them read a row of E scores per token.  A token belongs to a group of L neighbouring lanes, each of which holds V scores as
+// pieces of 16 bytes, piece p of lane i being number p L + i of the row: every load instruction of a group covers whole lines, and
+// every reduction over a row is one inside registers and log2(L) cross-lane moves.  V is 16 beyond 8 experts: few cross-lane steps
+// (each costs as much as one over all registers), and 64 / L tokens of a wave share the instructions of what follows.
 #include "lanes.hpp"
 
 namespace grouter {
@@ -22,143 +23,340 @@ __device__ __forceinline__ float sigmoid_of(float x, float shift = 0.f) {
 }
 __device__ __forceinline__ float reciprocal_or_zero(float z) { return z == 0.f ? 0.f : 1.f / z; }
 
-// V consecutive scores of a row from column e0 on; what lies behind column E is not touched.
-template <class Type, int V>
-struct Scores {
-    typename Type::stored raw[V];
-    __device__ __forceinline__ void load(const typename Type::stored* __restrict__ row, int e0, int E, bool whole_pieces) {
-        if (whole_pieces && e0 + V <= E) {
-            typedef uint32_t Piece __attribute__((ext_vector_type(4)));
-            constexpr int n = V * sizeof(typename Type::stored) / 16;
-            Piece p[n];
+template <class Type>
+constexpr int kPiece = 16 / sizeof(typename Type::stored);
+
+// What a lane holds of a row: N pieces of W columns.  A piece that would reach behind column E is fetched from earlier columns, so that
+// only the row's own elements are read, and its first `skip` elements count as absent (they belong to the piece before).  Rows
+// shorter than a piece are fetched one by one.  Addresses need no more than the elements' own alignment.
+template <class Type, int L, int V>
+struct Row {
+    static constexpr int W = kPiece<Type>, N = V / W;
+    typename Type::stored raw[N][W];
+    int from[N], skip[N], end;     // columns from .. from + W - 1, elements skip .. end - 1 present
+    __device__ __forceinline__ void place(int part, int E) {
+        end = min(E, W);
 #pragma unroll
-            for (int i = 0; i < n; ++i) p[i] = reinterpret_cast<const Piece*>(row + e0)[i];
-            __builtin_memcpy(raw, p, sizeof(raw));
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) raw[v] = e0 + v < E ? row[e0 + v] : typename Type::stored(0);
+        for (int p = 0; p < N; ++p) {
+            const int start = (p * L + part) * W;
+            from[p] = max(0, min(start, E - W));
+            skip[p] = min(start - from[p], W);
         }
     }
-    __device__ __forceinline__ float operator[](int v) const { return Type::widen(raw[v]); }
+    __device__ __forceinline__ void load(const typename Type::stored* __restrict__ row, int E) {
+#pragma unroll
+        for (int p = 0; p < N; ++p) {
+            if (E >= W) {
+                __builtin_memcpy(raw[p], row + from[p], 16);
+            } else {
+#pragma unroll
+                for (int w = 0; w < W; ++w) raw[p][w] = w < E ? row[w] : typename Type::stored(0);
+            }
+        }
+    }
+    __device__ __forceinline__ bool has(int p, int w) const { return w >= skip[p] && w < end; }
+    __device__ __forceinline__ float at(int p, int w) const { return Type::widen(raw[p][w]); }
 };
 
-// A whole number that orders like the score: NaN like -inf, -0 like +0; 0 is below all of them (a score taken already, or none).
+// ---- keys: whole numbers, all different within a row, that order like the scores and among equal scores by the lower column -------
+// A score's bits become a two's complement number (-0 and +0 both 0), moved up by the distance of the largest positive NaN from the
+// largest number, so that positive NaNs wrap round to the far end and a maximum with -inf's number sends all NaNs to -inf.  The
+// column, inverted, stands below it: 16-bit scores fill a 32-bit key, 32-bit scores the upper bits of a positive double, for which
+// the hardware has a maximum and a minimum in one instruction each.
 template <class Type>
-__device__ __forceinline__ uint32_t order_of(typename Type::stored raw) {
-    uint32_t b = __float_as_uint(Type::widen(raw));
-    b = (b & 0x7fffffffu) > 0x7f800000u ? 0xff800000u : b;
-    b = b == 0x80000000u ? 0u : b;
-    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+struct Keys16 {
+    typedef int32_t Key;
+    static constexpr uint16_t kInf = Type::kInf, kMove = 0x7fff - kInf;
+    static __device__ __forceinline__ Key none() { return INT32_MIN; }
+    static __device__ __forceinline__ void make(const uint16_t* raw, int column, Key* out) {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        typedef int16_t s16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            u16x2 u;
+            __builtin_memcpy(&u, raw + i, 4);
+            const s16x2 sign = __builtin_bit_cast(s16x2, u) >> 15;
+            const u16x2 s = __builtin_bit_cast(u16x2, sign);
+            const u16x2 t = ((u & (uint16_t)0x7fff) ^ s) + ((u16x2)(kMove) - s);
+            const s16x2 k = __builtin_elementwise_max(__builtin_bit_cast(s16x2, t), (s16x2)((int16_t)(kMove - kInf)));
+            const uint32_t word = __builtin_bit_cast(uint32_t, k);
+            out[i] = (int32_t)(word << 16 | (uint32_t)(0xffff - column - i));
+            out[i + 1] = (int32_t)((word & 0xffff0000u) | (uint32_t)(0xffff - column - i - 1));
+        }
+    }
+    static __device__ __forceinline__ int column(Key k) { return 0xffff - (k & 0xffff); }
+    // the score; -inf also where it was NaN
+    static __device__ __forceinline__ float score(Key k) {
+        const int v = (k >> 16) - kMove;
+        return Type::widen((uint16_t)((v < 0 ? -v : v) | (v < 0 ? 0x8000 : 0)));
+    }
+    static __device__ __forceinline__ Key larger(Key a, Key b) { return max(a, b); }
+    static __device__ __forceinline__ Key smaller(Key a, Key b) { return min(a, b); }
+    template <int STEP>
+    static __device__ __forceinline__ Key from_partner(Key k) { return (Key)partner<STEP>((uint32_t)k); }
+};
+struct Keys32 {
+    typedef double Key;
+    static constexpr uint32_t kInf = 0x7f800000u, kMove = 0x7fffffffu - kInf;
+    static __device__ __forceinline__ Key none() { return 0.0; }
+    static __device__ __forceinline__ void make(const float* raw, int column, Key* out) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t b = __float_as_uint(raw[i]), s = (uint32_t)((int32_t)b >> 31);
+            const int32_t k = max((int32_t)(((b & 0x7fffffffu) ^ s) + (kMove - s)), (int32_t)(kMove - kInf));
+            const uint32_t u = (uint32_t)k ^ 0x80000000u;
+            out[i] = __builtin_bit_cast(double, (uint64_t)u << 30 | (uint32_t)(0x3ff - column - i));
+        }
+    }
+    static __device__ __forceinline__ int column(Key k) { return 0x3ff - (int)(__builtin_bit_cast(uint64_t, k) & 0x3ffu); }
+    static __device__ __forceinline__ float score(Key k) {
+        const int32_t v = (int32_t)((uint32_t)(__builtin_bit_cast(uint64_t, k) >> 30) ^ 0x80000000u) - (int32_t)kMove;
+        return __uint_as_float((uint32_t)(v < 0 ? -v : v) | (v < 0 ? 0x80000000u : 0u));
+    }
+    static __device__ __forceinline__ Key larger(Key a, Key b) { return __builtin_fmax(a, b); }
+    static __device__ __forceinline__ Key smaller(Key a, Key b) { return __builtin_fmin(a, b); }
+    template <int STEP>
+    static __device__ __forceinline__ Key from_partner(Key k) {
+        const uint64_t b = __builtin_bit_cast(uint64_t, k);
+        return __builtin_bit_cast(double, (uint64_t)partner<STEP>((uint32_t)(b >> 32)) << 32 | partner<STEP>((uint32_t)b));
+    }
+};
+template <class Type> struct KeysOf { typedef Keys16<Type> type; };
+template <> struct KeysOf<Fp32> { typedef Keys32 type; };
+
+template <class K, int A, int B, int N>
+__device__ __forceinline__ void exchange(typename K::Key (&x)[N]) {
+    const auto a = x[A], b = x[B];
+    x[A] = K::larger(a, b);
+    x[B] = K::smaller(a, b);
+}
+template <class K>
+__device__ __forceinline__ void sort_list(typename K::Key (&x)[4]) {   // largest first
+    exchange<K, 0, 2>(x); exchange<K, 1, 3>(x);
+    exchange<K, 0, 1>(x); exchange<K, 2, 3>(x);
+    exchange<K, 1, 2>(x);
+}
+template <class K>
+__device__ __forceinline__ void sort_list(typename K::Key (&x)[8]) {
+    exchange<K, 0, 2>(x); exchange<K, 1, 3>(x); exchange<K, 4, 6>(x); exchange<K, 5, 7>(x);
+    exchange<K, 0, 4>(x); exchange<K, 1, 5>(x); exchange<K, 2, 6>(x); exchange<K, 3, 7>(x);
+    exchange<K, 0, 1>(x); exchange<K, 2, 3>(x); exchange<K, 4, 5>(x); exchange<K, 6, 7>(x);
+    exchange<K, 2, 4>(x); exchange<K, 3, 5>(x);
+    exchange<K, 1, 4>(x); exchange<K, 3, 6>(x);
+    exchange<K, 1, 2>(x); exchange<K, 3, 4>(x); exchange<K, 5, 6>(x);
+}
+// x becomes the largest of two lists, each sorted: the larger of x[i] and y[last - i] are they, and rise and fall once
+template <class K>
+__device__ __forceinline__ void merge_list(typename K::Key (&x)[4], const typename K::Key (&y)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = K::larger(x[i], y[3 - i]);
+    exchange<K, 0, 2>(x); exchange<K, 1, 3>(x);
+    exchange<K, 0, 1>(x); exchange<K, 2, 3>(x);
+}
+template <class K>
+__device__ __forceinline__ void merge_list(typename K::Key (&x)[8], const typename K::Key (&y)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = K::larger(x[i], y[7 - i]);
+    exchange<K, 0, 4>(x); exchange<K, 1, 5>(x); exchange<K, 2, 6>(x); exchange<K, 3, 7>(x);
+    exchange<K, 0, 2>(x); exchange<K, 1, 3>(x); exchange<K, 4, 6>(x); exchange<K, 5, 7>(x);
+    exchange<K, 0, 1>(x); exchange<K, 2, 3>(x); exchange<K, 4, 5>(x); exchange<K, 6, 7>(x);
+}
+template <class K, int L, int M, int STEP = 1>
+__device__ __forceinline__ void merge_group(typename K::Key (&x)[M]) {
+    if constexpr (STEP < L) {
+        typename K::Key y[M];
+#pragma unroll
+        for (int i = 0; i < M; ++i) y[i] = K::template from_partner<STEP>(x[i]);
+        merge_list<K>(x, y);
+        merge_group<K, L, M, 2 * STEP>(x);
+    }
+}
+template <class K, int L, int STEP = 1>
+__device__ __forceinline__ typename K::Key largest_of_group(typename K::Key k) {
+    if constexpr (STEP >= L) return k;
+    else return largest_of_group<K, L, 2 * STEP>(K::larger(k, K::template from_partner<STEP>(k)));
 }
 
-template <class IdxT>
-__device__ __forceinline__ int id_at(const void* ids, int64_t i) { return (int)((const IdxT*)ids)[i]; }
-__device__ __forceinline__ int id_of(const void* ids, int idx_dtype, int64_t i) {
-    return idx_dtype == 1 ? id_at<uint8_t>(ids, i) : id_at<int32_t>(ids, i);
-}
+struct RouteOut {
+    void* ids;
+    int idx_dtype;
+    uint16_t* gates;
+    __device__ __forceinline__ void put(int64_t i, int id, float gate) const {
+        gates[i] = Bf16::narrow(gate);
+        if (idx_dtype == 1) ((uint8_t*)ids)[i] = (uint8_t)id;
+        else ((int32_t*)ids)[i] = id;
+    }
+};
 
-// Ids and gates.  k rounds: the largest remaining order number of the group, the first lane that holds it (lanes hold ascending
-// columns, so on ties the lowest expert), and there the first place.
 template <class Type, int L, int V>
-__global__ __launch_bounds__(kThreads) void k_route(const typename Type::stored* __restrict__ scores, int64_t ld, bool whole_pieces,
-                                                    int64_t T, int E, int k, int gating, const uint8_t* __restrict__ token_mask,
-                                                    void* __restrict__ ids, int idx_dtype, uint16_t* __restrict__ gates) {
+__device__ __forceinline__ float exp_sum(const Row<Type, L, V>& x, float top) {
+    float z = 0.f;
+#pragma unroll
+    for (int p = 0; p < x.N; ++p)
+#pragma unroll
+        for (int w = 0; w < x.W; ++w) z += x.has(p, w) ? exp_of(x.at(p, w) - top) : 0.f;
+    return group_sum<L>(z);
+}
+
+// The weight of a picked score before it is divided by the sum over what its gate is a share of.
+__device__ __forceinline__ float gate_weight(int gating, float s, float top) { return gating >= kSigmoid ? sigmoid_of(s, top) : exp_of(s - top); }
+__device__ __forceinline__ float gate_shift(int gating, float largest) {
+    return gating == kSigmoid ? 0.f : shift_of(gating == kSigmoidNormalised ? fminf(largest, 0.f) : largest);
+}
+
+// Ids and gates, k <= M.  A lane sorts its keys in lists of M, merges them to their M largest, and log2(L) more merges with its partners'
+// lists leave every lane of the group with the row's.  No branch, no memory in between: for 128 experts, k = 8 and 16-bit scores about
+// 25 of the 60 instructions per token; k rounds of a maximum over the group take twice as many.
+template <class Type, int L, int V, int M>
+__global__ __launch_bounds__(kThreads) void k_route_lists(const typename Type::stored* __restrict__ scores, int64_t ld, int64_t T, int E, int k,
+                                                          int gating, const uint8_t* __restrict__ token_mask, RouteOut out) {
+    typedef typename KeysOf<Type>::type K;
+    typedef typename K::Key Key;
+    const int part = threadIdx.x % L;
+    const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
+    const bool here = t < T;
+    const auto* row = scores + (here ? t : T - 1) * ld;
+    Row<Type, L, V> x;
+    x.place(part, E);
+    x.load(row, E);
+    const bool masked = token_mask && here && token_mask[t] == 0;
+    Key keys[V];
+#pragma unroll
+    for (int p = 0; p < x.N; ++p) {
+        K::make(x.raw[p], x.from[p], keys + p * x.W);
+#pragma unroll
+        for (int w = 0; w < x.W; ++w) keys[p * x.W + w] = x.has(p, w) ? keys[p * x.W + w] : K::none();
+    }
+    Key list[M];
+#pragma unroll
+    for (int a = 0; a < V; a += M) {
+        Key next[M];
+#pragma unroll
+        for (int i = 0; i < M; ++i) next[i] = keys[a + i];
+        sort_list<K>(next);
+        if (a == 0) {
+#pragma unroll
+            for (int i = 0; i < M; ++i) list[i] = next[i];
+        } else {
+            merge_list<K>(list, next);
+        }
+    }
+    merge_group<K, L, M>(list);
+    // slot j of the row to lane j % L
+    constexpr int S = (M + L - 1) / L;
+    const float top = gate_shift(gating, K::score(list[0]));
+    float weight[S], z = 0.f;
+    int column[S];
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+        Key mine = list[i * L];
+#pragma unroll
+        for (int j = 1; j < L && i * L + j < M; ++j) mine = part == j ? list[i * L + j] : mine;
+        const int j = i * L + part;
+        column[i] = j < k ? K::column(mine) : 0;
+        float s = K::score(mine);
+        if (j < k && s == -INFINITY) s = Type::widen(row[column[i]]);     // or NaN, which ranks with it
+        weight[i] = j < k ? gate_weight(gating, s, top) : 0.f;
+        z += weight[i];
+    }
+    z = gating == kSoftmaxAll ? exp_sum(x, top) : group_sum<L>(z);
+    const float scale = gating == kSigmoid ? 1.f : reciprocal_or_zero(z);
+    if (!here) return;
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+        if (i * L + part < k) out.put(t * k + i * L + part, column[i], masked ? 0.f : weight[i] * scale);
+}
+
+// Ids and gates for any k: k rounds, each of which takes the largest key left in the group.
+template <class Type, int L, int V>
+__global__ __launch_bounds__(kThreads) void k_route_rounds(const typename Type::stored* __restrict__ scores, int64_t ld, int64_t T, int E, int k,
+                                                           int gating, const uint8_t* __restrict__ token_mask, RouteOut out) {
+    typedef typename KeysOf<Type>::type K;
+    typedef typename K::Key Key;
     extern __shared__ uint16_t s_pick[];
-    const int lane = threadIdx.x & 63, part = lane % L, e0 = part * V;
-    const int local = threadIdx.x / L;
+    const int part = threadIdx.x % L, local = threadIdx.x / L;
     const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + local;
     const bool here = t < T;
     const auto* row = scores + (here ? t : T - 1) * ld;
     uint16_t* pick = s_pick + local * k;
-    Scores<Type, V> x;
-    x.load(row, e0, E, whole_pieces);
-    uint32_t order[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) order[v] = e0 + v < E ? order_of<Type>(x.raw[v]) : 0u;
-    float top = -INFINITY, z = 0.f;
-    if (gating == kSoftmaxAll) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) top = e0 + v < E ? fmaxf(top, x[v]) : top;
-        top = shift_of(group_max<L>(top));
-#pragma unroll
-        for (int v = 0; v < V; ++v) z += e0 + v < E ? exp_of(x[v] - top) : 0.f;
-        z = group_sum<L>(z);
-    }
-    const int first = lane - part;
-    for (int j = 0; j < k; ++j) {
-        uint32_t best = order[0];
-#pragma unroll
-        for (int v = 1; v < V; ++v) best = max(best, order[v]);
-        const uint32_t most = group_max<L>(best);
-        const uint64_t holders = __ballot(best == most) >> first;
-        if (best == most && (holders & ((1ull << part) - 1)) == 0) {
-            bool found = false;
-            int at = 0;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const bool hit = !found && order[v] == most;
-                at = hit ? v : at;
-                order[v] = hit ? 0u : order[v];
-                found = found || hit;
-            }
-            pick[j] = (uint16_t)(e0 + at);
-        }
-    }
-    __syncthreads();
-    // the picked scores, one per lane and round, read again from the row that has just been fetched
+    Row<Type, L, V> x;
+    x.place(part, E);
+    x.load(row, E);
     const bool masked = token_mask && here && token_mask[t] == 0;
-    if (gating == kSoftmaxSelected) top = shift_of(Type::widen(row[pick[0]]));
-    if (gating == kSigmoid) top = 0.f;
-    if (gating == kSigmoidNormalised) top = shift_of(fminf(Type::widen(row[pick[0]]), 0.f));
-    auto weight = [&](int j) {
-        const float s = Type::widen(row[pick[j]]);
-        return gating >= kSigmoid ? sigmoid_of(s, top) : exp_of(s - top);
-    };
-    if (gating == kSoftmaxSelected || gating == kSigmoidNormalised) {
-        for (int j = part; j < k; j += L) z += weight(j);
+    Key keys[V];
+#pragma unroll
+    for (int p = 0; p < x.N; ++p) {
+        K::make(x.raw[p], x.from[p], keys + p * x.W);
+#pragma unroll
+        for (int w = 0; w < x.W; ++w) keys[p * x.W + w] = x.has(p, w) ? keys[p * x.W + w] : K::none();
+    }
+    float top = 0.f;
+    for (int j = 0; j < k; ++j) {
+        Key best = keys[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) best = K::larger(best, keys[v]);
+        best = largest_of_group<K, L>(best);
+#pragma unroll
+        for (int v = 0; v < V; ++v) keys[v] = keys[v] == best ? K::none() : keys[v];
+        if (j == 0) top = gate_shift(gating, K::score(best));
+        if (part == j % L) pick[j] = (uint16_t)K::column(best);     // read again by this lane alone
+    }
+    float z = 0.f;
+    if (gating == kSoftmaxAll) {
+        z = exp_sum(x, top);
+    } else {
+        for (int j = part; j < k; j += L) z += gate_weight(gating, Type::widen(row[pick[j]]), top);
         z = group_sum<L>(z);
     }
-    const float scale = masked ? 0.f : gating == kSigmoid ? 1.f : reciprocal_or_zero(z);
+    const float scale = gating == kSigmoid ? 1.f : reciprocal_or_zero(z);
     if (!here) return;
-    for (int j = part; j < k; j += L) {
-        const float g = masked ? 0.f : weight(j) * scale;
-        gates[t * k + j] = Bf16::narrow(g);
-        if (idx_dtype == 1) ((uint8_t*)ids)[t * k + j] = (uint8_t)pick[j];
-        else ((int32_t*)ids)[t * k + j] = (int32_t)pick[j];
-    }
+    for (int j = part; j < k; j += L) out.put(t * k + j, pick[j], masked ? 0.f : gate_weight(gating, Type::widen(row[pick[j]]), top) * scale);
 }
 
-// How many of the S + 1 ascending offsets are at most t; sequence s holds the tokens [off[s], off[s + 1]).
+__device__ __forceinline__ int id_of(const void* ids, int idx_dtype, int64_t i) {
+    return idx_dtype == 1 ? (int)((const uint8_t*)ids)[i] : (int)((const int32_t*)ids)[i];
+}
+
+// How many of the S + 1 ascending offsets are at most t, t the same in all lanes: 64 probes at a time.  Sequence s holds the tokens
+// [off[s], off[s + 1]).
 __device__ __forceinline__ int64_t offsets_up_to(const int64_t* __restrict__ off, int64_t S, int64_t t) {
+    const int lane = threadIdx.x & 63;
     int64_t lo = 0, hi = S + 1;
     while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (off[mid] <= t) lo = mid + 1;
-        else hi = mid;
+        const int64_t step = (hi - lo + 63) / 64, probe = lo + (lane + 1) * step - 1;
+        const int passed = __popcll(__ballot(probe < hi && off[min(probe, S)] <= t));
+        lo += passed * step;
+        hi = min(hi, lo + step - 1);
     }
     return lo;
 }
 
-// Probabilities over all experts of a row, from what a lane holds: softmax, or sigmoids over their sum.  Zero behind column E.
+// Probabilities over all experts of a row, from what a lane holds: softmax, or sigmoids over their sum.  Zero where the lane holds nothing.
 template <class Type, int L, int V>
-__device__ __forceinline__ void probabilities(const Scores<Type, V>& x, int e0, int E, bool sigmoid, float* p) {
+__device__ __forceinline__ void probabilities(const Row<Type, L, V>& x, bool sigmoid, float (&prob)[V]) {
     float top = -INFINITY, z = 0.f;
 #pragma unroll
-    for (int v = 0; v < V; ++v) top = e0 + v < E ? fmaxf(top, x[v]) : top;
+    for (int p = 0; p < x.N; ++p)
+#pragma unroll
+        for (int w = 0; w < x.W; ++w) {
+            prob[p * x.W + w] = x.has(p, w) ? x.at(p, w) : -INFINITY;
+            top = fmaxf(top, prob[p * x.W + w]);
+        }
     top = group_max<L>(top);
-    top = shift_of(sigmoid ? fminf(top, 0.f) : top);
     if (sigmoid) {
+        top = shift_of(fminf(top, 0.f));
 #pragma unroll
-        for (int v = 0; v < V; ++v) p[v] = e0 + v < E ? sigmoid_of(x[v], top) : 0.f;
+        for (int v = 0; v < V; ++v) prob[v] = sigmoid_of(prob[v], top);
     } else {
+        top = shift_of(top);
 #pragma unroll
-        for (int v = 0; v < V; ++v) p[v] = e0 + v < E ? exp_of(x[v] - top) : 0.f;
+        for (int v = 0; v < V; ++v) prob[v] = exp_of(prob[v] - top);
     }
 #pragma unroll
-    for (int v = 0; v < V; ++v) z += p[v];
+    for (int v = 0; v < V; ++v) z += prob[v];
     const float scale = reciprocal_or_zero(group_sum<L>(z));
 #pragma unroll
-    for (int v = 0; v < V; ++v) p[v] *= scale;
+    for (int v = 0; v < V; ++v) prob[v] *= scale;
 }
 
 struct RouteGrad {
@@ -174,9 +372,19 @@ struct RouteGrad {
     int64_t out_ld;
 };
 
-__device__ __forceinline__ void store_as(void* out, int dtype, int64_t i, float v) {
-    if (dtype == 0) ((float*)out)[i] = v;
-    else ((uint16_t*)out)[i] = dtype == 1 ? Bf16::narrow(v) : Fp16::narrow(v);
+template <class Out, int W>
+__device__ __forceinline__ void store_piece(void* out, int64_t at, int skip, int end, const float* v) {
+    auto* o = (typename Out::stored*)out + at;
+    typename Out::stored q[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w) q[w] = Out::narrow(v[w]);
+    if (skip == 0 && end == W) {
+        __builtin_memcpy(o, q, sizeof(q));
+    } else {
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            if (w >= skip && w < end) o[w] = q[w];
+    }
 }
 
 // Gradient by the scores.  With p the probabilities over all experts, g the gates, q the gradients by the gates' logs and c the
@@ -184,41 +392,61 @@ __device__ __forceinline__ void store_as(void* out, int dtype, int64_t i, float 
 // (softmax over them), q_j and everywhere -p_e sum q (softmax over all), (1 - sigmoid) q_j or (1 - sigmoid) (q_j - g_j sum q).
 // Nothing is divided by a gate, so a gate of 0 has a gradient of 0.  WHOLE: the row's scores are needed, not the picked ones alone.
 template <class Type, int L, int V, bool WHOLE>
-__global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::stored* __restrict__ scores, int64_t ld, bool whole_pieces,
-                                                        int64_t T, int E, int gating, RouteGrad a) {
+__global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::stored* __restrict__ scores, int64_t ld, int64_t T, int E, int gating,
+                                                        RouteGrad a) {
     extern __shared__ float s_slot[];    // per token k contributions, then k expert numbers
-    const int lane = threadIdx.x & 63, part = lane % L, e0 = part * V;
-    const int local = threadIdx.x / L;
+    constexpr int W = kPiece<Type>, N = V / W;
+    const int part = threadIdx.x % L, local = threadIdx.x / L;
     const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + local;
     const bool here = t < T, live = here && !(a.token_mask && a.token_mask[t] == 0);
     const auto* row = scores + (here ? t : T - 1) * ld;
     const bool sigmoid = gating >= kSigmoid;
-    float ds[V], p[V];
-    Scores<Type, V> x;
+    float ds[V], prob[V];
+    Row<Type, L, V> x;
+    x.place(part, E);
 #pragma unroll
     for (int v = 0; v < V; ++v) ds[v] = 0.f;
-    if (WHOLE) {
-        x.load(row, e0, E, whole_pieces);
-        probabilities<Type, L, V>(x, e0, E, sigmoid, p);
-    }
-    if (WHOLE && a.coef) {
-        int64_t s = a.off ? offsets_up_to(a.off, a.S, t) - 1 : 0;
-        if (s >= a.S) s = -1;     // behind the last sequence, as before the first: in none
-        float c[V], dot = 0.f;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            c[v] = s >= 0 && e0 + v < E ? a.coef[s * E + e0 + v] : 0.f;
-            dot += c[v] * p[v];
+    if (WHOLE) x.load(row, E);
+    int64_t s = 0;
+    if (WHOLE && a.off) {
+        // the sequence of the wave's first token is most often that of all its tokens
+        const int64_t first = (int64_t)blockIdx.x * (kThreads / L) + (threadIdx.x & ~63) / L, last = first + 64 / L - 1;
+        s = offsets_up_to(a.off, a.S, first);
+        if (s <= a.S && a.off[s] <= last) {
+            int64_t hi = a.S + 1;
+            while (s < hi) {
+                const int64_t mid = (s + hi) >> 1;
+                if (a.off[mid] <= t) s = mid + 1;
+                else hi = mid;
+            }
         }
+        s = s > a.S ? -1 : s - 1;     // behind the last sequence, as before the first: in none
+    }
+    if (WHOLE) probabilities<Type, L, V>(x, sigmoid, prob);
+    if (WHOLE && a.coef) {
+        float c[V], dot = 0.f;
+        const float* coef = a.coef + (s >= 0 ? s : 0) * E;
+#pragma unroll
+        for (int p = 0; p < N; ++p) {
+            if (E >= W) {
+                __builtin_memcpy(c + p * W, coef + x.from[p], W * sizeof(float));
+            } else {
+#pragma unroll
+                for (int w = 0; w < W; ++w) c[p * W + w] = w < E ? coef[w] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) dot += c[v] * prob[v];
         dot = group_sum<L>(dot);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            ds[v] = s >= 0 ? p[v] * (c[v] - dot) : 0.f;
-            if (sigmoid) ds[v] *= s >= 0 ? sigmoid_of(-x[v]) : 0.f;
+            ds[v] = s >= 0 ? prob[v] * (c[v] - dot) : 0.f;
+            if (sigmoid) ds[v] *= s >= 0 ? sigmoid_of(-x.at(v / W, v % W)) : 0.f;
         }
     }
     if (a.dlog) {
         const int k = a.k;
+        const bool shared = gating == kSoftmaxSelected || gating == kSigmoidNormalised;
         float* u = s_slot + local * 2 * k;
         int* e = (int*)(u + k);
         float sum = 0.f, top = -INFINITY, z = 0.f;
@@ -228,36 +456,45 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
             e[j] = ok ? id : -1;
             u[j] = ok ? a.dlog[t * k + j] : 0.f;
             sum += u[j];
-            if (ok && (gating == kSoftmaxSelected || gating == kSigmoidNormalised)) top = fmaxf(top, Type::widen(row[id]));
+            if (ok && shared) top = fmaxf(top, Type::widen(row[id]));
         }
         sum = group_sum<L>(sum);
-        if (gating == kSoftmaxSelected || gating == kSigmoidNormalised) {
-            top = group_max<L>(top);
-            top = shift_of(sigmoid ? fminf(top, 0.f) : top);
+        if (shared) {
+            top = gate_shift(gating, group_max<L>(top));
             for (int j = part; j < k; j += L)
-                if (e[j] >= 0) z += sigmoid ? sigmoid_of(Type::widen(row[e[j]]), top) : exp_of(Type::widen(row[e[j]]) - top);
+                if (e[j] >= 0) z += gate_weight(gating, Type::widen(row[e[j]]), top);
             const float scale = sum * reciprocal_or_zero(group_sum<L>(z));
             for (int j = part; j < k; j += L)
-                if (e[j] >= 0) u[j] -= scale * (sigmoid ? sigmoid_of(Type::widen(row[e[j]]), top) : exp_of(Type::widen(row[e[j]]) - top));
+                if (e[j] >= 0) u[j] -= scale * gate_weight(gating, Type::widen(row[e[j]]), top);
         }
         if (sigmoid)
             for (int j = part; j < k; j += L)
                 if (e[j] >= 0) u[j] *= sigmoid_of(-Type::widen(row[e[j]]));
-        if (WHOLE && gating == kSoftmaxAll)
+        if (WHOLE && gating == kSoftmaxAll) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) ds[v] -= p[v] * sum;
+            for (int v = 0; v < V; ++v) ds[v] -= prob[v] * sum;
+        }
         __syncthreads();
         for (int j = 0; j < k; ++j) {
-            const int at = e[j] - e0;
+            const int id = e[j];
             const float w = u[j];
 #pragma unroll
-            for (int v = 0; v < V; ++v) ds[v] += at == v ? w : 0.f;
+            for (int v = 0; v < V; ++v) ds[v] += id == x.from[v / W] + v % W ? w : 0.f;
         }
     }
     if (!here) return;
+    if (!live) {
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (e0 + v < E) store_as(a.out, a.out_dtype, t * a.out_ld + e0 + v, live ? ds[v] : 0.f);
+        for (int v = 0; v < V; ++v) ds[v] = 0.f;
+    }
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+        const int64_t at = t * a.out_ld + x.from[p];
+        if (x.skip[p] >= x.end) continue;
+        if (a.out_dtype == 0) store_piece<Fp32, W>(a.out, at, x.skip[p], x.end, ds + p * W);
+        else if (a.out_dtype == 1) store_piece<Bf16, W>(a.out, at, x.skip[p], x.end, ds + p * W);
+        else store_piece<Fp16, W>(a.out, at, x.skip[p], x.end, ds + p * W);
+    }
 }
 
 // ---- balance loss -------------------------------------------------------------------------------------------------------------
@@ -265,50 +502,60 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
 // coef_e = alpha E f_e / n.  The tokens are cut into chunks of equal length, one per workgroup; the part of a sequence inside a chunk
 // leaves its sums in a slot of its own, chunk + sequence (both only grow along the tokens, so no two parts share one), and a second
 // launch adds up each sequence's slots in order.  So work is even whatever the sequences' lengths, and no float is added atomically.
+struct BalanceCell {
+    float prob;
+    int32_t count;
+};
 struct BalanceParts {
-    float* sum;       // [chunks + S][E]
-    int32_t* count;   // [chunks + S][E]
-    int32_t* tokens;  // [chunks + S]
-    double* loss;     // [S]
-    uint32_t* done;   // sequences finished
-    int64_t rows;     // of a chunk
+    BalanceCell* cells;  // [chunks + S][E]
+    int32_t* tokens;     // [chunks + S], valid ones
+    double* loss;        // [S][column blocks]
+    uint32_t* done;      // workgroups that have left their loss
+    int64_t rows;        // of a chunk
 };
 
+constexpr int kPartThreads = 512;
+
 template <class Type, int L, int V>
-__global__ __launch_bounds__(kThreads) void k_balance_parts(const typename Type::stored* __restrict__ scores, int64_t ld, bool whole_pieces,
-                                                            int64_t T, int E, int k, bool sigmoid, const uint8_t* __restrict__ token_mask,
-                                                            const void* __restrict__ ids, int idx_dtype,
-                                                            const int64_t* __restrict__ off, int64_t S, BalanceParts parts) {
-    __shared__ float s_sum[kThreads / 64][L * V];
+__global__ __launch_bounds__(kPartThreads) void k_balance_parts(const typename Type::stored* __restrict__ scores, int64_t ld, int64_t T, int E, int k,
+                                                                bool sigmoid, const uint8_t* __restrict__ token_mask,
+                                                                const void* __restrict__ ids, int idx_dtype,
+                                                                const int64_t* __restrict__ off, int64_t S, BalanceParts parts) {
+    constexpr int W = kPiece<Type>, kWaves = kPartThreads / 64, kTokens = kPartThreads / L;
+    __shared__ float s_sum[kWaves][L * V];
     __shared__ int s_count[L * V];
     __shared__ int s_tokens;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane % L, e0 = part * V;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane % L;
     const int64_t row0 = blockIdx.x * parts.rows, row1 = min(T, row0 + parts.rows);
     if (blockIdx.x == 0 && threadIdx.x == 0) *parts.done = 0;
+    Row<Type, L, V> x, ahead;
+    x.place(part, E);
     for (int64_t s = off ? max((int64_t)0, offsets_up_to(off, S, row0) - 1) : 0; s < S; ++s) {
         const int64_t begin = off ? off[s] : 0, end = off ? off[s + 1] : T;
         if (begin >= row1) break;
         const int64_t a = max(begin, row0), b = min(end, row1);
         if (a >= b) continue;
-        for (int e = threadIdx.x; e < E; e += kThreads) s_count[e] = 0;
+        for (int e = threadIdx.x; e < E; e += kPartThreads) s_count[e] = 0;
         if (threadIdx.x == 0) s_tokens = 0;
         __syncthreads();
         float sum[V];
         int tokens = 0;
 #pragma unroll
         for (int v = 0; v < V; ++v) sum[v] = 0.f;
-        for (int64_t t0 = a; t0 < b; t0 += kThreads / L) {
+        ahead = x;
+        ahead.load(scores + min(a + threadIdx.x / L, b - 1) * ld, E);
+        for (int64_t t0 = a; t0 < b; t0 += kTokens) {
             const int64_t t = t0 + threadIdx.x / L;
+            x = ahead;
+            ahead.load(scores + min(t + kTokens, b - 1) * ld, E);
             const bool live = t < b && !(token_mask && token_mask[t] == 0);
-            Scores<Type, V> x;
-            x.load(scores + (t < b ? t : b - 1) * ld, e0, E, whole_pieces);
             float p[V];
-            probabilities<Type, L, V>(x, e0, E, sigmoid, p);
+            probabilities<Type, L, V>(x, sigmoid, p);
 #pragma unroll
             for (int v = 0; v < V; ++v) sum[v] += live ? p[v] : 0.f;
             tokens += live;
         }
-        for (int64_t i = a * k + threadIdx.x; i < b * k; i += kThreads) {
+        for (int64_t i = a * k + threadIdx.x; i < b * k; i += kPartThreads) {
             const int id = id_of(ids, idx_dtype, i);
             if ((unsigned)id < (unsigned)E && !(token_mask && token_mask[i / k] == 0)) atomicAdd(&s_count[id], 1);
         }
@@ -316,96 +563,110 @@ __global__ __launch_bounds__(kThreads) void k_balance_parts(const typename Type:
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             for (int step = L; step < 64; step *= 2) sum[v] += __shfl_xor(sum[v], step);
-            if (lane < L) s_sum[wave][e0 + v] = sum[v];
+            if (lane < L && x.has(v / W, v % W)) s_sum[wave][x.from[v / W] + v % W] = sum[v];
         }
         __syncthreads();
         const int64_t slot = blockIdx.x + s;
-        for (int e = threadIdx.x; e < E; e += kThreads) {
+        for (int e = threadIdx.x; e < E; e += kPartThreads) {
             float all = 0.f;
 #pragma unroll
-            for (int w = 0; w < kThreads / 64; ++w) all += s_sum[w][e];
-            parts.sum[slot * E + e] = all;
-            parts.count[slot * E + e] = s_count[e];
+            for (int w = 0; w < kWaves; ++w) all += s_sum[w][e];
+            parts.cells[slot * E + e] = BalanceCell{all, s_count[e]};
         }
         if (threadIdx.x == 0) parts.tokens[slot] = s_tokens;
         __syncthreads();
     }
 }
 
-constexpr int kJoinThreads = 1024;
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+    for (int step = 32; step > 0; step /= 2) v += __shfl_xor(v, step);
+    return v;
+}
 
-__global__ __launch_bounds__(kJoinThreads) void k_balance_join(int64_t T, int E, int k, const int64_t* __restrict__ off, int64_t S,
-                                                               BalanceParts parts, float alpha, int32_t* __restrict__ counts,
-                                                               float* __restrict__ prob, float* __restrict__ coef, float* __restrict__ loss) {
-    __shared__ double s_sum[kJoinThreads];
-    __shared__ int s_count[kJoinThreads], s_tokens;
+// Joins the slots of one sequence for COLUMNS experts; THREADS / COLUMNS threads share the slots of an expert.
+template <int COLUMNS, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_balance_join(int64_t T, int E, int k, const uint8_t* __restrict__ token_mask,
+                                                          const int64_t* __restrict__ off, int64_t S, BalanceParts parts, float alpha,
+                                                          int32_t* __restrict__ counts, float* __restrict__ prob, float* __restrict__ coef,
+                                                          float* __restrict__ loss) {
+    constexpr int kWaves = THREADS / 64, kDeals = THREADS / COLUMNS;
+    __shared__ double s_sum[kWaves][COLUMNS];
+    __shared__ int s_count[kWaves][COLUMNS], s_tokens[kWaves];
     __shared__ bool s_last;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t s = blockIdx.x;
     const int64_t begin = off ? max((int64_t)0, off[s]) : 0, end = off ? min(T, off[s + 1]) : T;
     const int64_t c0 = begin / parts.rows, c1 = begin < end ? (end - 1) / parts.rows + 1 : c0;
-    if (threadIdx.x == 0) s_tokens = 0;
+    const int col = threadIdx.x % COLUMNS, e = blockIdx.y * COLUMNS + col;
+    double sum = 0.0;
+    int count = 0, tokens = 0;
+    if (e < E)
+#pragma unroll 8
+        for (int64_t c = c0 + threadIdx.x / COLUMNS; c < c1; c += kDeals) {
+            const BalanceCell cell = parts.cells[(c + s) * E + e];
+            sum += (double)cell.prob;
+            count += cell.count;
+        }
+    if (token_mask)
+        for (int64_t c = c0 + threadIdx.x; c < c1; c += THREADS) tokens += parts.tokens[c + s];
+#pragma unroll
+    for (int step = COLUMNS; step < 64; step *= 2) {
+        sum += __shfl_xor(sum, step);
+        count += __shfl_xor(count, step);
+    }
+    if (token_mask)
+#pragma unroll
+        for (int step = 1; step < 64; step *= 2) tokens += __shfl_xor(tokens, step);
+    if (lane < COLUMNS) {
+        s_sum[wave][lane] = sum;
+        s_count[wave][lane] = count;
+    }
+    if (lane == 0) s_tokens[wave] = tokens;
     __syncthreads();
-    int mine = 0;
-    for (int64_t c = c0 + threadIdx.x; c < c1; c += blockDim.x) mine += parts.tokens[c + s];
-    if (mine) atomicAdd(&s_tokens, mine);
-    // columns side by side, the slots dealt out over what threads are left
-    int width = 64;
-    while (width < E && width < (int)blockDim.x) width *= 2;
-    const int col = threadIdx.x % width, deal = threadIdx.x / width, deals = blockDim.x / width;
-    double total = 0.0;
-    for (int e0 = 0; e0 < E; e0 += width) {
-        const int e = e0 + col;
-        double sum = 0.0;
-        int count = 0;
-        if (e < E)
-#pragma unroll 4
-            for (int64_t c = c0 + deal; c < c1; c += deals) {
-                sum += (double)parts.sum[(c + s) * E + e];
-                count += parts.count[(c + s) * E + e];
+    if (wave == 0) {
+        double part = 0.0;
+        if (lane < COLUMNS) {
+            for (int w = 1; w < kWaves; ++w) {
+                sum += s_sum[w][lane];
+                count += s_count[w][lane];
             }
-        __syncthreads();
-        s_sum[threadIdx.x] = sum;
-        s_count[threadIdx.x] = count;
-        __syncthreads();
-        if (deal == 0 && e < E) {
-            for (int d = 1; d < deals; ++d) {
-                sum += s_sum[d * width + col];
-                count += s_count[d * width + col];
-            }
-            const double n = s_tokens > 0 ? (double)s_tokens : 1.0;
-            const double mean = sum / n, share = (double)count / (k * n);
+        }
+        if (token_mask) {
+            tokens = 0;
+            for (int w = 0; w < kWaves; ++w) tokens += s_tokens[w];
+        } else {
+            tokens = (int)max((int64_t)0, end - begin);
+        }
+        if (lane < COLUMNS && e < E) {
+            const double over = 1.0 / max(tokens, 1), mean = sum * over, scaled = (double)alpha * E / k * over * count;
             counts[s * E + e] = count;
             prob[s * E + e] = (float)mean;
-            coef[s * E + e] = (float)((double)alpha * E * share / n);
-            total += (double)alpha * E * share * mean;
+            coef[s * E + e] = (float)(scaled * over);
+            part = scaled * mean;
+        }
+        part = wave_sum(part);
+        if (gridDim.x == 1 && gridDim.y == 1) {
+            if (lane == 0) *loss = (float)part;
+        } else if (lane == 0) {
+            __hip_atomic_store(parts.loss + s * gridDim.y + blockIdx.y, part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            s_last = __hip_atomic_fetch_add(parts.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1 == gridDim.x * gridDim.y;
         }
     }
-    auto block_sum = [&](double v) {
-        __syncthreads();
-        s_sum[threadIdx.x] = v;
-        __syncthreads();
-        for (int step = blockDim.x / 2; step > 0; step /= 2) {
-            if ((int)threadIdx.x < step) s_sum[threadIdx.x] += s_sum[threadIdx.x + step];
-            __syncthreads();
-        }
-        return s_sum[0];
-    };
-    total = block_sum(total);
-    if (S == 1) {
-        if (threadIdx.x == 0) *loss = (float)total;
-        return;
-    }
-    // the workgroup that finishes last adds up the sequences' losses, in their order whichever it is
-    if (threadIdx.x == 0) {
-        __hip_atomic_store(parts.loss + s, total, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s_last = __hip_atomic_fetch_add(parts.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1 == (uint32_t)S;
-    }
+    if (gridDim.x == 1 && gridDim.y == 1) return;
     __syncthreads();
     if (!s_last) return;
+    // the workgroup that finishes last adds up all losses, in their order whichever it is
     double all = 0.0;
-    for (int64_t i = threadIdx.x; i < S; i += blockDim.x) all += __hip_atomic_load(parts.loss + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    all = block_sum(all);
-    if (threadIdx.x == 0) *loss = (float)all;
+    for (int64_t i = threadIdx.x; i < S * gridDim.y; i += THREADS) all += __hip_atomic_load(parts.loss + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    all = wave_sum(all);
+    __syncthreads();
+    if (lane == 0) s_sum[wave][0] = all;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kWaves; ++w) all += s_sum[w][0];
+        *loss = (float)all;
+    }
 }
 
 // Calls f with the lanes per token and the scores per lane that E experts take.
@@ -413,14 +674,19 @@ template <class F>
 hipError_t with_lanes(int E, F f) {
 #define GROUTER_LANES(L, V) return f(std::integral_constant<int, L>{}, std::integral_constant<int, V>{})
     if (E <= 8) GROUTER_LANES(1, 8);
-    if (E <= 16) GROUTER_LANES(2, 8);
-    if (E <= 32) GROUTER_LANES(4, 8);
-    if (E <= 64) GROUTER_LANES(8, 8);
-    if (E <= 128) GROUTER_LANES(16, 8);
-    if (E <= 256) GROUTER_LANES(32, 8);
-    if (E <= 512) GROUTER_LANES(64, 8);
+    if (E <= 16) GROUTER_LANES(1, 16);
+    if (E <= 32) GROUTER_LANES(2, 16);
+    if (E <= 64) GROUTER_LANES(4, 16);
+    if (E <= 128) GROUTER_LANES(8, 16);
+    if (E <= 256) GROUTER_LANES(16, 16);
+    if (E <= 512) GROUTER_LANES(32, 16);
     GROUTER_LANES(64, 16);
 #undef GROUTER_LANES
+}
+int lanes_of(int E) {
+    int l = 1;
+    while (l * 16 < E) l *= 2;
+    return l;
 }
 template <class F>
 hipError_t with_type(int dtype, F f) {
@@ -429,19 +695,20 @@ hipError_t with_type(int dtype, F f) {
     return f(Fp16{});
 }
 
-bool whole_pieces(const void* p, int64_t ld, int dtype) { return (((uintptr_t)p | (uintptr_t)(ld * (dtype == 0 ? 4 : 2))) & 15u) == 0; }
-
 }  // namespace
 
 hipError_t launch_route(const void* scores, int dtype, int64_t ld, int64_t T, int E, int k, int gating, const uint8_t* token_mask, void* ids,
                         int idx_dtype, uint16_t* gates, hipStream_t s) {
-    const bool whole = whole_pieces(scores, ld, dtype);
+    const RouteOut out{ids, idx_dtype, gates};
     return with_type(dtype, [&](auto type) {
         return with_lanes(E, [&](auto l, auto v) {
             typedef decltype(type) Type;
             constexpr int L = decltype(l)::value, V = decltype(v)::value, tokens = kThreads / L;
-            hipLaunchKernelGGL((k_route<Type, L, V>), dim3((unsigned)((T + tokens - 1) / tokens)), dim3(kThreads), tokens * k * sizeof(uint16_t), s,
-                               (const typename Type::stored*)scores, ld, whole, T, E, k, gating, token_mask, ids, idx_dtype, gates);
+            const dim3 grid((unsigned)((T + tokens - 1) / tokens)), threads(kThreads);
+            const auto* x = (const typename Type::stored*)scores;
+            if (k <= 4) hipLaunchKernelGGL((k_route_lists<Type, L, V, 4>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
+            else if (k <= 8) hipLaunchKernelGGL((k_route_lists<Type, L, V, 8>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
+            else hipLaunchKernelGGL((k_route_rounds<Type, L, V>), grid, threads, tokens * k * sizeof(uint16_t), s, x, ld, T, E, k, gating, token_mask, out);
             return hipGetLastError();
         });
     });
@@ -450,7 +717,6 @@ hipError_t launch_route(const void* scores, int dtype, int64_t ld, int64_t T, in
 hipError_t launch_route_bwd(const void* scores, int dtype, int64_t ld, int64_t T, int E, int gating, const uint8_t* token_mask, const void* ids,
                             int idx_dtype, int k, const float* dlog, const int64_t* off, int64_t S, const float* coef, void* out,
                             int out_dtype, int64_t out_ld, hipStream_t s) {
-    const bool whole = whole_pieces(scores, ld, dtype);
     const RouteGrad a{ids, idx_dtype, k, dlog, off, S, coef, token_mask, out, out_dtype, out_ld};
     return with_type(dtype, [&](auto type) {
         return with_lanes(E, [&](auto l, auto v) {
@@ -458,37 +724,27 @@ hipError_t launch_route_bwd(const void* scores, int dtype, int64_t ld, int64_t T
             constexpr int L = decltype(l)::value, V = decltype(v)::value, tokens = kThreads / L;
             const dim3 grid((unsigned)((T + tokens - 1) / tokens));
             const size_t lds = dlog ? tokens * k * 2 * sizeof(float) : 0;
-            if (coef || gating == kSoftmaxAll)
-                hipLaunchKernelGGL((k_route_bwd<Type, L, V, true>), grid, dim3(kThreads), lds, s, (const typename Type::stored*)scores, ld, whole,
-                                   T, E, gating, a);
-            else
-                hipLaunchKernelGGL((k_route_bwd<Type, L, V, false>), grid, dim3(kThreads), lds, s, (const typename Type::stored*)scores, ld, whole,
-                                   T, E, gating, a);
+            const auto* x = (const typename Type::stored*)scores;
+            if (coef || gating == kSoftmaxAll) hipLaunchKernelGGL((k_route_bwd<Type, L, V, true>), grid, dim3(kThreads), lds, s, x, ld, T, E, gating, a);
+            else hipLaunchKernelGGL((k_route_bwd<Type, L, V, false>), grid, dim3(kThreads), lds, s, x, ld, T, E, gating, a);
             return hipGetLastError();
         });
     });
 }
 
 // Chunks: a few per CU at most, so that a sequence's slots are few, and not below the tokens that a workgroup takes at a time.
-static int64_t balance_rows(int64_t T, int E) {
-    int64_t at_once = kThreads;
-    for (int e = 8; e < E && at_once > 4; e *= 2) at_once /= 2;
-    const int64_t rows = (T + 511) / 512;
-    return (rows + at_once - 1) / at_once * at_once;
-}
-
 BalanceLayout balance_layout(int64_t T, int E, int64_t S) {
     BalanceLayout l{};
-    l.rows = balance_rows(T, E);
+    const int64_t at_once = kPartThreads / lanes_of(E), rows = (T + 511) / 512;
+    l.rows = (rows + at_once - 1) / at_once * at_once;
     l.chunks = (T + l.rows - 1) / l.rows;
     const size_t slots = (size_t)(l.chunks + S);
     size_t o = 0;
     auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
     l.done = take(256);
-    l.loss = take(sizeof(double) * (size_t)S);
+    l.loss = take(sizeof(double) * (size_t)S * ((size_t)(E + 15) / 16));
     l.tokens = take(sizeof(int32_t) * slots);
-    l.sum = take(sizeof(float) * slots * (size_t)E);
-    l.count = take(sizeof(int32_t) * slots * (size_t)E);
+    l.cells = take(sizeof(BalanceCell) * slots * (size_t)E);
     l.total = o;
     return l;
 }
@@ -496,20 +752,25 @@ BalanceLayout balance_layout(int64_t T, int E, int64_t S) {
 hipError_t launch_balance(const void* scores, int dtype, int64_t ld, int64_t T, int E, int k, bool sigmoid, const uint8_t* token_mask, const void* ids,
                           int idx_dtype, const int64_t* off, int64_t S, float alpha, int32_t* counts, float* prob, float* coef,
                           float* loss, void* ws, hipStream_t s) {
-    const bool whole = whole_pieces(scores, ld, dtype);
     const BalanceLayout l = balance_layout(T, E, S);
     char* w = (char*)ws;
-    const BalanceParts parts{(float*)(w + l.sum), (int32_t*)(w + l.count), (int32_t*)(w + l.tokens), (double*)(w + l.loss), (uint32_t*)(w + l.done), l.rows};
+    const BalanceParts parts{(BalanceCell*)(w + l.cells), (int32_t*)(w + l.tokens), (double*)(w + l.loss), (uint32_t*)(w + l.done), l.rows};
     const hipError_t e = with_type(dtype, [&](auto type) {
         return with_lanes(E, [&](auto lanes, auto v) {
             typedef decltype(type) Type;
-            hipLaunchKernelGGL((k_balance_parts<Type, decltype(lanes)::value, decltype(v)::value>), dim3((unsigned)l.chunks), dim3(kThreads), 0, s,
-                               (const typename Type::stored*)scores, ld, whole, T, E, k, sigmoid, token_mask, ids, idx_dtype, off, S, parts);
+            hipLaunchKernelGGL((k_balance_parts<Type, decltype(lanes)::value, decltype(v)::value>), dim3((unsigned)l.chunks), dim3(kPartThreads), 0, s,
+                               (const typename Type::stored*)scores, ld, T, E, k, sigmoid, token_mask, ids, idx_dtype, off, S, parts);
             return hipGetLastError();
         });
     });
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_balance_join, dim3((unsigned)S), dim3(S == 1 ? kJoinThreads : 256), 0, s, T, E, k, off, S, parts, alpha, counts, prob, coef, loss);
+    // many slots per sequence: 64 threads to an expert's; few: 4
+    if (S < 8)
+        hipLaunchKernelGGL((k_balance_join<16, 1024>), dim3((unsigned)S, (unsigned)(E + 15) / 16), dim3(1024), 0, s, T, E, k, token_mask, off, S, parts,
+                           alpha, counts, prob, coef, loss);
+    else
+        hipLaunchKernelGGL((k_balance_join<64, 256>), dim3((unsigned)S, (unsigned)(E + 63) / 64), dim3(256), 0, s, T, E, k, token_mask, off, S, parts,
+                           alpha, counts, prob, coef, loss);
     return hipGetLastError();
 }
 
