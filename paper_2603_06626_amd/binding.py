@@ -426,20 +426,32 @@ def grouter_fold_weights(W_s, group_of, E_T, out, stream=None):
            "grouter_fold_weights")
 
 
-def _float_dtype(t, name, allowed=(FP32, BF16, FP16)):
-    import torch
+_FLOATS = {}     # torch dtype -> GROUTER_FP32 ..., filled when first asked
 
-    dt = {torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16}.get(t.dtype)
+
+def _float_dtype(t, name, allowed=(FP32, BF16, FP16)):
+    if not _FLOATS:
+        import torch
+
+        _FLOATS.update({torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16})
+    dt = _FLOATS.get(t.dtype)
     if dt not in allowed:
         raise ValueError(f"{name} has an unsupported dtype ({t.dtype})")
     return dt
 
 
 def _matrix(t, name):
-    """A GPU matrix whose rows are contiguous; its row stride may exceed its width."""
-    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        raise ValueError(f"{name} must be a GPU matrix with contiguous rows")
-    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+    """How far apart the rows of a GPU matrix are; a row is contiguous, its neighbours may be further off than its width."""
+    if t.is_cuda and t.dim() == 2:
+        E = t.shape[1]
+        if t.is_contiguous():
+            return E
+        rows, columns = t.stride()
+        if columns == 1 and rows >= E:
+            return rows
+        if E == 1 and rows >= 1:
+            return rows
+    raise ValueError(f"{name} must be a GPU matrix with contiguous rows")
 
 
 def _mask(token_mask, T):

@@ -317,14 +317,20 @@ __device__ __forceinline__ int id_of(const void* ids, int idx_dtype, int64_t i) 
     return idx_dtype == 1 ? (int)((const uint8_t*)ids)[i] : (int)((const int32_t*)ids)[i];
 }
 
-// How many of the S + 1 ascending offsets are at most t, t the same in all lanes: 64 probes at a time.  Sequence s holds the tokens
-// [off[s], off[s + 1]).
-__device__ __forceinline__ int64_t offsets_up_to(const int64_t* __restrict__ off, int64_t S, int64_t t) {
+// How many of the S + 1 ascending offsets are at most t, t the same in all lanes, and the offset after them (INT64_MAX behind the last):
+// 64 probes at a time, so up to 63 sequences take a single load.  Sequence s holds the tokens [off[s], off[s + 1]).
+__device__ __forceinline__ int64_t offsets_up_to(const int64_t* __restrict__ off, int64_t S, int64_t t, int64_t& next) {
     const int lane = threadIdx.x & 63;
     int64_t lo = 0, hi = S + 1;
+    next = INT64_MAX;
     while (lo < hi) {
         const int64_t step = (hi - lo + 63) / 64, probe = lo + (lane + 1) * step - 1;
-        const int passed = __popcll(__ballot(probe < hi && off[min(probe, S)] <= t));
+        const int64_t value = probe < hi ? off[probe] : INT64_MAX;
+        const int passed = __popcll(__ballot(value <= t));
+        if (passed < 64) {
+            const int64_t above = __shfl(value, passed);
+            if (above != INT64_MAX) next = above;     // else the one that an earlier round of probes found
+        }
         lo += passed * step;
         hi = min(hi, lo + step - 1);
     }
@@ -410,9 +416,10 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
     int64_t s = 0;
     if (WHOLE && a.off) {
         // the sequence of the wave's first token is most often that of all its tokens
-        const int64_t first = (int64_t)blockIdx.x * (kThreads / L) + (threadIdx.x & ~63) / L, last = first + 64 / L - 1;
-        s = offsets_up_to(a.off, a.S, first);
-        if (s <= a.S && a.off[s] <= last) {
+        const int64_t first = (int64_t)blockIdx.x * (kThreads / L) + (threadIdx.x & ~63) / L;
+        int64_t next;
+        s = offsets_up_to(a.off, a.S, first, next);
+        if (next < first + 64 / L) {
             int64_t hi = a.S + 1;
             while (s < hi) {
                 const int64_t mid = (s + hi) >> 1;
@@ -515,26 +522,66 @@ struct BalanceParts {
 };
 
 constexpr int kPartThreads = 512;
+constexpr int kAloneSequences = 4, kAloneRounds = 4;
 
-template <class Type, int L, int V>
+struct BalanceOut {
+    float alpha;
+    int32_t* counts;
+    float *prob, *coef, *loss;
+    // results of one expert in a sequence with these sums; its part of the loss
+    __device__ __forceinline__ double put(int64_t at, int E, int k, int tokens, double sum, int count) const {
+        const double over = 1.0 / max(tokens, 1), mean = sum * over, scaled = (double)alpha * E / k * over * count;
+        counts[at] = count;
+        prob[at] = (float)mean;
+        coef[at] = (float)(scaled * over);
+        return scaled * mean;
+    }
+};
+
+template <int STEP>
+__device__ __forceinline__ float rotated(float v) { return __uint_as_float(dpp_move<0x120 + STEP>(__float_as_uint(v))); }   // row_ror
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+    for (int step = 32; step > 0; step /= 2) v += __shfl_xor(v, step);
+    return v;
+}
+
+// ALONE: one workgroup takes all tokens and writes the results itself.
+template <class Type, int L, int V, bool ALONE>
 __global__ __launch_bounds__(kPartThreads) void k_balance_parts(const typename Type::stored* __restrict__ scores, int64_t ld, int64_t T, int E, int k,
                                                                 bool sigmoid, const uint8_t* __restrict__ token_mask,
                                                                 const void* __restrict__ ids, int idx_dtype,
-                                                                const int64_t* __restrict__ off, int64_t S, BalanceParts parts) {
-    constexpr int W = kPiece<Type>, kWaves = kPartThreads / 64, kTokens = kPartThreads / L;
-    __shared__ float s_sum[kWaves][L * V];
+                                                                const int64_t* __restrict__ off, int64_t S, BalanceParts parts, BalanceOut out) {
+    constexpr int kWaves = kPartThreads / 64, kTokens = kPartThreads / L;
+    constexpr int kRows = L <= 16 ? 4 : 64 / L;      // partial sums that a wave leaves in LDS: one per 16 lanes, or per group
+    __shared__ float s_sum[kWaves * kRows][L * V];
     __shared__ int s_count[L * V];
     __shared__ int s_tokens;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane % L;
     const int64_t row0 = blockIdx.x * parts.rows, row1 = min(T, row0 + parts.rows);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *parts.done = 0;
+    if (!ALONE && blockIdx.x == 0 && threadIdx.x == 0) *parts.done = 0;
+    double loss = 0.0;
     Row<Type, L, V> x, ahead;
     x.place(part, E);
-    for (int64_t s = off ? max((int64_t)0, offsets_up_to(off, S, row0) - 1) : 0; s < S; ++s) {
-        const int64_t begin = off ? off[s] : 0, end = off ? off[s + 1] : T;
-        if (begin >= row1) break;
-        const int64_t a = max(begin, row0), b = min(end, row1);
-        if (a >= b) continue;
+    // sequence s is [begin, next); -1 stands for the tokens before the first
+    int64_t s = 0, begin = 0, next = T;
+    if (off && ALONE) {
+        begin = off[0];
+        next = off[1];
+    } else if (off) {
+        s = offsets_up_to(off, S, row0, next) - 1;
+        begin = row0;
+    }
+    for (; s < S; ++s, begin = next, next = off && s < S ? off[s + 1] : T) {
+        if (!ALONE && begin >= row1) break;
+        const int64_t a = max(begin, row0), b = min(next, row1);
+        if (s < 0) continue;
+        if (a >= b) {
+            if (ALONE)
+                for (int e = threadIdx.x; e < E; e += kPartThreads) out.put(s * E + e, E, k, 0, 0.0, 0);
+            continue;
+        }
         for (int e = threadIdx.x; e < E; e += kPartThreads) s_count[e] = 0;
         if (threadIdx.x == 0) s_tokens = 0;
         __syncthreads();
@@ -544,52 +591,62 @@ __global__ __launch_bounds__(kPartThreads) void k_balance_parts(const typename T
         for (int v = 0; v < V; ++v) sum[v] = 0.f;
         ahead = x;
         ahead.load(scores + min(a + threadIdx.x / L, b - 1) * ld, E);
+        const uint32_t slots = (uint32_t)(b - a) * (uint32_t)k;
+#pragma unroll 4
+        for (uint32_t i = threadIdx.x; i < slots; i += kPartThreads) {
+            const int id = id_of(ids, idx_dtype, a * k + i);
+            if ((unsigned)id < (unsigned)E && !(token_mask && token_mask[a + i / (uint32_t)k] == 0)) atomicAdd(&s_count[id], 1);
+        }
         for (int64_t t0 = a; t0 < b; t0 += kTokens) {
             const int64_t t = t0 + threadIdx.x / L;
             x = ahead;
-            ahead.load(scores + min(t + kTokens, b - 1) * ld, E);
             const bool live = t < b && !(token_mask && token_mask[t] == 0);
+            tokens += live;
+            if (t0 + kTokens < b) ahead.load(scores + min(t + kTokens, b - 1) * ld, E);
             float p[V];
             probabilities<Type, L, V>(x, sigmoid, p);
 #pragma unroll
             for (int v = 0; v < V; ++v) sum[v] += live ? p[v] : 0.f;
-            tokens += live;
-        }
-        for (int64_t i = a * k + threadIdx.x; i < b * k; i += kPartThreads) {
-            const int id = id_of(ids, idx_dtype, i);
-            if ((unsigned)id < (unsigned)E && !(token_mask && token_mask[i / k] == 0)) atomicAdd(&s_count[id], 1);
         }
         if (part == 0 && tokens) atomicAdd(&s_tokens, tokens);
+        // over the groups within 16 lanes in registers, over the rest in LDS
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            for (int step = L; step < 64; step *= 2) sum[v] += __shfl_xor(sum[v], step);
-            if (lane < L && x.has(v / W, v % W)) s_sum[wave][x.from[v / W] + v % W] = sum[v];
+            if constexpr (L <= 1) sum[v] += rotated<1>(sum[v]);
+            if constexpr (L <= 2) sum[v] += rotated<2>(sum[v]);
+            if constexpr (L <= 4) sum[v] += rotated<4>(sum[v]);
+            if constexpr (L <= 8) sum[v] += rotated<8>(sum[v]);
+            constexpr int kSpan = 64 / kRows;
+            if (lane % kSpan < L && x.has(v / x.W, v % x.W)) s_sum[wave * kRows + lane / kSpan][x.from[v / x.W] + v % x.W] = sum[v];
         }
         __syncthreads();
         const int64_t slot = blockIdx.x + s;
         for (int e = threadIdx.x; e < E; e += kPartThreads) {
             float all = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) all += s_sum[w][e];
-            parts.cells[slot * E + e] = BalanceCell{all, s_count[e]};
+            for (int w = 0; w < kWaves * kRows; ++w) all += s_sum[w][e];
+            if (ALONE) loss += out.put(s * E + e, E, k, s_tokens, all, s_count[e]);
+            else parts.cells[slot * E + e] = BalanceCell{all, s_count[e]};
         }
-        if (threadIdx.x == 0) parts.tokens[slot] = s_tokens;
+        if (!ALONE && threadIdx.x == 0) parts.tokens[slot] = s_tokens;
         __syncthreads();
     }
-}
-
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-    for (int step = 32; step > 0; step /= 2) v += __shfl_xor(v, step);
-    return v;
+    if (ALONE) {
+        __shared__ double s_loss[kWaves];
+        loss = wave_sum(loss);
+        if (lane == 0) s_loss[wave] = loss;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int w = 1; w < kWaves; ++w) loss += s_loss[w];
+            *out.loss = (float)loss;
+        }
+    }
 }
 
 // Joins the slots of one sequence for COLUMNS experts; THREADS / COLUMNS threads share the slots of an expert.
 template <int COLUMNS, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_balance_join(int64_t T, int E, int k, const uint8_t* __restrict__ token_mask,
-                                                          const int64_t* __restrict__ off, int64_t S, BalanceParts parts, float alpha,
-                                                          int32_t* __restrict__ counts, float* __restrict__ prob, float* __restrict__ coef,
-                                                          float* __restrict__ loss) {
+                                                          const int64_t* __restrict__ off, int64_t S, BalanceParts parts, BalanceOut out) {
     constexpr int kWaves = THREADS / 64, kDeals = THREADS / COLUMNS;
     __shared__ double s_sum[kWaves][COLUMNS];
     __shared__ int s_count[kWaves][COLUMNS], s_tokens[kWaves];
@@ -638,16 +695,10 @@ __global__ __launch_bounds__(THREADS) void k_balance_join(int64_t T, int E, int 
         } else {
             tokens = (int)max((int64_t)0, end - begin);
         }
-        if (lane < COLUMNS && e < E) {
-            const double over = 1.0 / max(tokens, 1), mean = sum * over, scaled = (double)alpha * E / k * over * count;
-            counts[s * E + e] = count;
-            prob[s * E + e] = (float)mean;
-            coef[s * E + e] = (float)(scaled * over);
-            part = scaled * mean;
-        }
+        if (lane < COLUMNS && e < E) part = out.put(s * E + e, E, k, tokens, sum, count);
         part = wave_sum(part);
         if (gridDim.x == 1 && gridDim.y == 1) {
-            if (lane == 0) *loss = (float)part;
+            if (lane == 0) *out.loss = (float)part;
         } else if (lane == 0) {
             __hip_atomic_store(parts.loss + s * gridDim.y + blockIdx.y, part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             s_last = __hip_atomic_fetch_add(parts.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1 == gridDim.x * gridDim.y;
@@ -665,7 +716,7 @@ __global__ __launch_bounds__(THREADS) void k_balance_join(int64_t T, int E, int 
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int w = 1; w < kWaves; ++w) all += s_sum[w][0];
-        *loss = (float)all;
+        *out.loss = (float)all;
     }
 }
 
@@ -755,22 +806,29 @@ hipError_t launch_balance(const void* scores, int dtype, int64_t ld, int64_t T, 
     const BalanceLayout l = balance_layout(T, E, S);
     char* w = (char*)ws;
     const BalanceParts parts{(BalanceCell*)(w + l.cells), (int32_t*)(w + l.tokens), (double*)(w + l.loss), (uint32_t*)(w + l.done), l.rows};
+    const BalanceOut out{alpha, counts, prob, coef, loss};
+    // one workgroup and no second launch where it needs few rounds: see kAloneRounds
+    const bool alone = S <= kAloneSequences && T <= (int64_t)kAloneRounds * kPartThreads / lanes_of(E);
+    BalanceParts whole = parts;
+    if (alone) whole.rows = T;
     const hipError_t e = with_type(dtype, [&](auto type) {
         return with_lanes(E, [&](auto lanes, auto v) {
             typedef decltype(type) Type;
-            hipLaunchKernelGGL((k_balance_parts<Type, decltype(lanes)::value, decltype(v)::value>), dim3((unsigned)l.chunks), dim3(kPartThreads), 0, s,
-                               (const typename Type::stored*)scores, ld, T, E, k, sigmoid, token_mask, ids, idx_dtype, off, S, parts);
+            constexpr int L = decltype(lanes)::value, V = decltype(v)::value;
+            const auto* x = (const typename Type::stored*)scores;
+            if (alone) hipLaunchKernelGGL((k_balance_parts<Type, L, V, true>), dim3(1), dim3(kPartThreads), 0, s, x, ld, T, E, k, sigmoid, token_mask, ids,
+                                          idx_dtype, off, S, whole, out);
+            else hipLaunchKernelGGL((k_balance_parts<Type, L, V, false>), dim3((unsigned)l.chunks), dim3(kPartThreads), 0, s, x, ld, T, E, k, sigmoid,
+                                    token_mask, ids, idx_dtype, off, S, parts, out);
             return hipGetLastError();
         });
     });
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || alone) return e;
     // many slots per sequence: 64 threads to an expert's; few: 4
     if (S < 8)
-        hipLaunchKernelGGL((k_balance_join<16, 1024>), dim3((unsigned)S, (unsigned)(E + 15) / 16), dim3(1024), 0, s, T, E, k, token_mask, off, S, parts,
-                           alpha, counts, prob, coef, loss);
+        hipLaunchKernelGGL((k_balance_join<16, 1024>), dim3((unsigned)S, (unsigned)(E + 15) / 16), dim3(1024), 0, s, T, E, k, token_mask, off, S, parts, out);
     else
-        hipLaunchKernelGGL((k_balance_join<64, 256>), dim3((unsigned)S, (unsigned)(E + 63) / 64), dim3(256), 0, s, T, E, k, token_mask, off, S, parts,
-                           alpha, counts, prob, coef, loss);
+        hipLaunchKernelGGL((k_balance_join<64, 256>), dim3((unsigned)S, (unsigned)(E + 63) / 64), dim3(256), 0, s, T, E, k, token_mask, off, S, parts, out);
     return hipGetLastError();
 }
 
