@@ -28,33 +28,38 @@ constexpr int kPiece = 16 / sizeof(typename Type::stored);
 
 // What a lane holds of a row: N pieces of W columns.  A piece that would reach behind column E is fetched from earlier columns, so that
 // only the row's own elements are read, and its first `skip` elements count as absent (they belong to the piece before).  Rows
-// shorter than a piece are fetched one by one.  Addresses need no more than the elements' own alignment.
-template <class Type, int L, int V>
+// shorter than a piece are fetched one by one.  Addresses need no more than the elements' own alignment.  FULL: E = L V, nothing is
+// absent and nothing has to be compared for it.
+template <class Type, int L, int V, bool FULL>
 struct Row {
     static constexpr int W = kPiece<Type>, N = V / W;
+    static constexpr bool kShort = L == 1 && V == 8 && !FULL;     // E may be less than a piece
     typename Type::stored raw[N][W];
     int from[N], skip[N], end;     // columns from .. from + W - 1, elements skip .. end - 1 present
     __device__ __forceinline__ void place(int part, int E) {
-        end = min(E, W);
+        end = kShort ? min(E, W) : W;
 #pragma unroll
         for (int p = 0; p < N; ++p) {
             const int start = (p * L + part) * W;
-            from[p] = max(0, min(start, E - W));
-            skip[p] = min(start - from[p], W);
+            from[p] = FULL ? start : max(0, min(start, E - W));
+            skip[p] = FULL ? 0 : min(start - from[p], W);
+        }
+    }
+    // W elements of a row of anything, where the lane's piece p is
+    template <class T>
+    __device__ __forceinline__ void fetch(int p, const T* __restrict__ row, int E, T* out) const {
+        if (kShort && E < W) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) out[w] = w < E ? row[w] : T(0);
+        } else {
+            __builtin_memcpy(out, row + from[p], W * sizeof(T));
         }
     }
     __device__ __forceinline__ void load(const typename Type::stored* __restrict__ row, int E) {
 #pragma unroll
-        for (int p = 0; p < N; ++p) {
-            if (E >= W) {
-                __builtin_memcpy(raw[p], row + from[p], 16);
-            } else {
-#pragma unroll
-                for (int w = 0; w < W; ++w) raw[p][w] = w < E ? row[w] : typename Type::stored(0);
-            }
-        }
+        for (int p = 0; p < N; ++p) fetch(p, row, E, raw[p]);
     }
-    __device__ __forceinline__ bool has(int p, int w) const { return w >= skip[p] && w < end; }
+    __device__ __forceinline__ bool has(int p, int w) const { return FULL || (w >= skip[p] && (!kShort || w < end)); }
     __device__ __forceinline__ float at(int p, int w) const { return Type::widen(raw[p][w]); }
 };
 
@@ -188,8 +193,8 @@ struct RouteOut {
     }
 };
 
-template <class Type, int L, int V>
-__device__ __forceinline__ float exp_sum(const Row<Type, L, V>& x, float top) {
+template <class Type, int L, int V, bool FULL>
+__device__ __forceinline__ float exp_sum(const Row<Type, L, V, FULL>& x, float top) {
     float z = 0.f;
 #pragma unroll
     for (int p = 0; p < x.N; ++p)
@@ -207,7 +212,7 @@ __device__ __forceinline__ float gate_shift(int gating, float largest) {
 // Ids and gates, k <= M.  A lane sorts its keys in lists of M, merges them to their M largest, and log2(L) more merges with its partners'
 // lists leave every lane of the group with the row's.  No branch, no memory in between: for 128 experts, k = 8 and 16-bit scores about
 // 25 of the 60 instructions per token; k rounds of a maximum over the group take twice as many.
-template <class Type, int L, int V, int M>
+template <class Type, int L, int V, bool FULL, int M>
 __global__ __launch_bounds__(kThreads) void k_route_lists(const typename Type::stored* __restrict__ scores, int64_t ld, int64_t T, int E, int k,
                                                           int gating, const uint8_t* __restrict__ token_mask, RouteOut out) {
     typedef typename KeysOf<Type>::type K;
@@ -216,7 +221,7 @@ __global__ __launch_bounds__(kThreads) void k_route_lists(const typename Type::s
     const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
     const bool here = t < T;
     const auto* row = scores + (here ? t : T - 1) * ld;
-    Row<Type, L, V> x;
+    Row<Type, L, V, FULL> x;
     x.place(part, E);
     x.load(row, E);
     const bool masked = token_mask && here && token_mask[t] == 0;
@@ -268,7 +273,7 @@ __global__ __launch_bounds__(kThreads) void k_route_lists(const typename Type::s
 }
 
 // Ids and gates for any k: k rounds, each of which takes the largest key left in the group.
-template <class Type, int L, int V>
+template <class Type, int L, int V, bool FULL>
 __global__ __launch_bounds__(kThreads) void k_route_rounds(const typename Type::stored* __restrict__ scores, int64_t ld, int64_t T, int E, int k,
                                                            int gating, const uint8_t* __restrict__ token_mask, RouteOut out) {
     typedef typename KeysOf<Type>::type K;
@@ -279,7 +284,7 @@ __global__ __launch_bounds__(kThreads) void k_route_rounds(const typename Type::
     const bool here = t < T;
     const auto* row = scores + (here ? t : T - 1) * ld;
     uint16_t* pick = s_pick + local * k;
-    Row<Type, L, V> x;
+    Row<Type, L, V, FULL> x;
     x.place(part, E);
     x.load(row, E);
     const bool masked = token_mask && here && token_mask[t] == 0;
@@ -338,8 +343,8 @@ __device__ __forceinline__ int64_t offsets_up_to(const int64_t* __restrict__ off
 }
 
 // Probabilities over all experts of a row, from what a lane holds: softmax, or sigmoids over their sum.  Zero where the lane holds nothing.
-template <class Type, int L, int V>
-__device__ __forceinline__ void probabilities(const Row<Type, L, V>& x, bool sigmoid, float (&prob)[V]) {
+template <bool SIGMOID, class Type, int L, int V, bool FULL>
+__device__ __forceinline__ void probabilities(const Row<Type, L, V, FULL>& x, float (&prob)[V]) {
     float top = -INFINITY, z = 0.f;
 #pragma unroll
     for (int p = 0; p < x.N; ++p)
@@ -349,7 +354,7 @@ __device__ __forceinline__ void probabilities(const Row<Type, L, V>& x, bool sig
             top = fmaxf(top, prob[p * x.W + w]);
         }
     top = group_max<L>(top);
-    if (sigmoid) {
+    if (SIGMOID) {
         top = shift_of(fminf(top, 0.f));
 #pragma unroll
         for (int v = 0; v < V; ++v) prob[v] = sigmoid_of(prob[v], top);
@@ -397,7 +402,7 @@ __device__ __forceinline__ void store_piece(void* out, int64_t at, int skip, int
 // balance loss's coefficients: p_e (c_e - <c, p>) (times 1 - sigmoid(s_e) for sigmoids), plus at the picked experts q_j - g_j sum q
 // (softmax over them), q_j and everywhere -p_e sum q (softmax over all), (1 - sigmoid) q_j or (1 - sigmoid) (q_j - g_j sum q).
 // Nothing is divided by a gate, so a gate of 0 has a gradient of 0.  WHOLE: the row's scores are needed, not the picked ones alone.
-template <class Type, int L, int V, bool WHOLE>
+template <class Type, int L, int V, bool FULL, bool WHOLE, bool SIGMOID>
 __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::stored* __restrict__ scores, int64_t ld, int64_t T, int E, int gating,
                                                         RouteGrad a) {
     extern __shared__ float s_slot[];    // per token k contributions, then k expert numbers
@@ -406,9 +411,9 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
     const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + local;
     const bool here = t < T, live = here && !(a.token_mask && a.token_mask[t] == 0);
     const auto* row = scores + (here ? t : T - 1) * ld;
-    const bool sigmoid = gating >= kSigmoid;
+    constexpr bool sigmoid = SIGMOID;
     float ds[V], prob[V];
-    Row<Type, L, V> x;
+    Row<Type, L, V, FULL> x;
     x.place(part, E);
 #pragma unroll
     for (int v = 0; v < V; ++v) ds[v] = 0.f;
@@ -429,18 +434,13 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
         }
         s = s > a.S ? -1 : s - 1;     // behind the last sequence, as before the first: in none
     }
-    if (WHOLE) probabilities<Type, L, V>(x, sigmoid, prob);
+    if (WHOLE) probabilities<SIGMOID>(x, prob);
     if (WHOLE && a.coef) {
         float c[V], dot = 0.f;
         const float* coef = a.coef + (s >= 0 ? s : 0) * E;
 #pragma unroll
         for (int p = 0; p < N; ++p) {
-            if (E >= W) {
-                __builtin_memcpy(c + p * W, coef + x.from[p], W * sizeof(float));
-            } else {
-#pragma unroll
-                for (int w = 0; w < W; ++w) c[p * W + w] = w < E ? coef[w] : 0.f;
-            }
+            x.fetch(p, coef, E, c + p * W);
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) dot += c[v] * prob[v];
@@ -497,10 +497,11 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
 #pragma unroll
     for (int p = 0; p < N; ++p) {
         const int64_t at = t * a.out_ld + x.from[p];
-        if (x.skip[p] >= x.end) continue;
-        if (a.out_dtype == 0) store_piece<Fp32, W>(a.out, at, x.skip[p], x.end, ds + p * W);
-        else if (a.out_dtype == 1) store_piece<Bf16, W>(a.out, at, x.skip[p], x.end, ds + p * W);
-        else store_piece<Fp16, W>(a.out, at, x.skip[p], x.end, ds + p * W);
+        const int skip = FULL ? 0 : x.skip[p], end = FULL ? W : x.end;
+        if (skip >= end) continue;
+        if (a.out_dtype == 0) store_piece<Fp32, W>(a.out, at, skip, end, ds + p * W);
+        else if (a.out_dtype == 1) store_piece<Bf16, W>(a.out, at, skip, end, ds + p * W);
+        else store_piece<Fp16, W>(a.out, at, skip, end, ds + p * W);
     }
 }
 
@@ -548,9 +549,9 @@ __device__ __forceinline__ double wave_sum(double v) {
 }
 
 // ALONE: one workgroup takes all tokens and writes the results itself.
-template <class Type, int L, int V, bool ALONE>
+template <class Type, int L, int V, bool FULL, bool SIGMOID, bool ALONE>
 __global__ __launch_bounds__(kPartThreads) void k_balance_parts(const typename Type::stored* __restrict__ scores, int64_t ld, int64_t T, int E, int k,
-                                                                bool sigmoid, const uint8_t* __restrict__ token_mask,
+                                                                const uint8_t* __restrict__ token_mask,
                                                                 const void* __restrict__ ids, int idx_dtype,
                                                                 const int64_t* __restrict__ off, int64_t S, BalanceParts parts, BalanceOut out) {
     constexpr int kWaves = kPartThreads / 64, kTokens = kPartThreads / L;
@@ -562,7 +563,7 @@ __global__ __launch_bounds__(kPartThreads) void k_balance_parts(const typename T
     const int64_t row0 = blockIdx.x * parts.rows, row1 = min(T, row0 + parts.rows);
     if (!ALONE && blockIdx.x == 0 && threadIdx.x == 0) *parts.done = 0;
     double loss = 0.0;
-    Row<Type, L, V> x, ahead;
+    Row<Type, L, V, FULL> x, ahead;
     x.place(part, E);
     // sequence s is [begin, next); -1 stands for the tokens before the first
     int64_t s = 0, begin = 0, next = T;
@@ -604,7 +605,7 @@ __global__ __launch_bounds__(kPartThreads) void k_balance_parts(const typename T
             tokens += live;
             if (t0 + kTokens < b) ahead.load(scores + min(t + kTokens, b - 1) * ld, E);
             float p[V];
-            probabilities<Type, L, V>(x, sigmoid, p);
+            probabilities<SIGMOID>(x, p);
 #pragma unroll
             for (int v = 0; v < V; ++v) sum[v] += live ? p[v] : 0.f;
         }
@@ -720,20 +721,29 @@ __global__ __launch_bounds__(THREADS) void k_balance_join(int64_t T, int E, int 
     }
 }
 
-// Calls f with the lanes per token and the scores per lane that E experts take.
+template <bool B>
+struct Flag {
+    static constexpr bool value = B;
+};
+// Calls f with the lanes per token and the scores per lane that E experts take, and whether E fills them.
 template <class F>
 hipError_t with_lanes(int E, F f) {
-#define GROUTER_LANES(L, V) return f(std::integral_constant<int, L>{}, std::integral_constant<int, V>{})
-    if (E <= 8) GROUTER_LANES(1, 8);
-    if (E <= 16) GROUTER_LANES(1, 16);
-    if (E <= 32) GROUTER_LANES(2, 16);
-    if (E <= 64) GROUTER_LANES(4, 16);
-    if (E <= 128) GROUTER_LANES(8, 16);
-    if (E <= 256) GROUTER_LANES(16, 16);
-    if (E <= 512) GROUTER_LANES(32, 16);
+#define GROUTER_LANES(L, V)                                                                                         \
+    if (E == L * V) return f(std::integral_constant<int, L>{}, std::integral_constant<int, V>{}, Flag<true>{});     \
+    if (E < L * V) return f(std::integral_constant<int, L>{}, std::integral_constant<int, V>{}, Flag<false>{})
+    GROUTER_LANES(1, 8);
+    GROUTER_LANES(1, 16);
+    GROUTER_LANES(2, 16);
+    GROUTER_LANES(4, 16);
+    GROUTER_LANES(8, 16);
+    GROUTER_LANES(16, 16);
+    GROUTER_LANES(32, 16);
     GROUTER_LANES(64, 16);
 #undef GROUTER_LANES
+    return hipErrorInvalidValue;
 }
+template <class F>
+hipError_t with_flag(bool b, F f) { return b ? f(Flag<true>{}) : f(Flag<false>{}); }
 int lanes_of(int E) {
     int l = 1;
     while (l * 16 < E) l *= 2;
@@ -752,14 +762,15 @@ hipError_t launch_route(const void* scores, int dtype, int64_t ld, int64_t T, in
                         int idx_dtype, uint16_t* gates, hipStream_t s) {
     const RouteOut out{ids, idx_dtype, gates};
     return with_type(dtype, [&](auto type) {
-        return with_lanes(E, [&](auto l, auto v) {
+        return with_lanes(E, [&](auto l, auto v, auto full) {
             typedef decltype(type) Type;
             constexpr int L = decltype(l)::value, V = decltype(v)::value, tokens = kThreads / L;
+            constexpr bool FULL = decltype(full)::value;
             const dim3 grid((unsigned)((T + tokens - 1) / tokens)), threads(kThreads);
             const auto* x = (const typename Type::stored*)scores;
-            if (k <= 4) hipLaunchKernelGGL((k_route_lists<Type, L, V, 4>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
-            else if (k <= 8) hipLaunchKernelGGL((k_route_lists<Type, L, V, 8>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
-            else hipLaunchKernelGGL((k_route_rounds<Type, L, V>), grid, threads, tokens * k * sizeof(uint16_t), s, x, ld, T, E, k, gating, token_mask, out);
+            if (k <= 4) hipLaunchKernelGGL((k_route_lists<Type, L, V, FULL, 4>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
+            else if (k <= 8) hipLaunchKernelGGL((k_route_lists<Type, L, V, FULL, 8>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
+            else hipLaunchKernelGGL((k_route_rounds<Type, L, V, FULL>), grid, threads, tokens * k * sizeof(uint16_t), s, x, ld, T, E, k, gating, token_mask, out);
             return hipGetLastError();
         });
     });
@@ -770,15 +781,21 @@ hipError_t launch_route_bwd(const void* scores, int dtype, int64_t ld, int64_t T
                             int out_dtype, int64_t out_ld, hipStream_t s) {
     const RouteGrad a{ids, idx_dtype, k, dlog, off, S, coef, token_mask, out, out_dtype, out_ld};
     return with_type(dtype, [&](auto type) {
-        return with_lanes(E, [&](auto l, auto v) {
+        return with_lanes(E, [&](auto l, auto v, auto full) {
             typedef decltype(type) Type;
             constexpr int L = decltype(l)::value, V = decltype(v)::value, tokens = kThreads / L;
+            constexpr bool FULL = decltype(full)::value;
             const dim3 grid((unsigned)((T + tokens - 1) / tokens));
             const size_t lds = dlog ? tokens * k * 2 * sizeof(float) : 0;
             const auto* x = (const typename Type::stored*)scores;
-            if (coef || gating == kSoftmaxAll) hipLaunchKernelGGL((k_route_bwd<Type, L, V, true>), grid, dim3(kThreads), lds, s, x, ld, T, E, gating, a);
-            else hipLaunchKernelGGL((k_route_bwd<Type, L, V, false>), grid, dim3(kThreads), lds, s, x, ld, T, E, gating, a);
-            return hipGetLastError();
+            return with_flag(gating >= kSigmoid, [&](auto sigmoid) {
+                constexpr bool SIGMOID = decltype(sigmoid)::value;
+                if (coef || gating == kSoftmaxAll)
+                    hipLaunchKernelGGL((k_route_bwd<Type, L, V, FULL, true, SIGMOID>), grid, dim3(kThreads), lds, s, x, ld, T, E, gating, a);
+                else
+                    hipLaunchKernelGGL((k_route_bwd<Type, L, V, FULL, false, SIGMOID>), grid, dim3(kThreads), lds, s, x, ld, T, E, gating, a);
+                return hipGetLastError();
+            });
         });
     });
 }
@@ -812,15 +829,20 @@ hipError_t launch_balance(const void* scores, int dtype, int64_t ld, int64_t T, 
     BalanceParts whole = parts;
     if (alone) whole.rows = T;
     const hipError_t e = with_type(dtype, [&](auto type) {
-        return with_lanes(E, [&](auto lanes, auto v) {
-            typedef decltype(type) Type;
-            constexpr int L = decltype(lanes)::value, V = decltype(v)::value;
-            const auto* x = (const typename Type::stored*)scores;
-            if (alone) hipLaunchKernelGGL((k_balance_parts<Type, L, V, true>), dim3(1), dim3(kPartThreads), 0, s, x, ld, T, E, k, sigmoid, token_mask, ids,
-                                          idx_dtype, off, S, whole, out);
-            else hipLaunchKernelGGL((k_balance_parts<Type, L, V, false>), dim3((unsigned)l.chunks), dim3(kPartThreads), 0, s, x, ld, T, E, k, sigmoid,
-                                    token_mask, ids, idx_dtype, off, S, parts, out);
-            return hipGetLastError();
+        return with_lanes(E, [&](auto lanes, auto v, auto full) {
+            return with_flag(sigmoid, [&](auto flag) {
+                typedef decltype(type) Type;
+                constexpr int L = decltype(lanes)::value, V = decltype(v)::value;
+                constexpr bool FULL = decltype(full)::value, SIGMOID = decltype(flag)::value;
+                const auto* x = (const typename Type::stored*)scores;
+                if (alone)
+                    hipLaunchKernelGGL((k_balance_parts<Type, L, V, FULL, SIGMOID, true>), dim3(1), dim3(kPartThreads), 0, s, x, ld, T, E, k, token_mask,
+                                       ids, idx_dtype, off, S, whole, out);
+                else
+                    hipLaunchKernelGGL((k_balance_parts<Type, L, V, FULL, SIGMOID, false>), dim3((unsigned)l.chunks), dim3(kPartThreads), 0, s, x, ld, T, E,
+                                       k, token_mask, ids, idx_dtype, off, S, parts, out);
+                return hipGetLastError();
+            });
         });
     });
     if (e != hipSuccess || alone) return e;
