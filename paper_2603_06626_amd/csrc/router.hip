@@ -60,6 +60,11 @@ struct Row {
         for (int p = 0; p < N; ++p) fetch(p, row, E, raw[p]);
     }
     __device__ __forceinline__ bool has(int p, int w) const { return FULL || (w >= skip[p] && (!kShort || w < end)); }
+    // where column e stands when all lanes' pieces are put side by side: in the last piece that is not whole, behind the absent ones
+    static __device__ __forceinline__ int place_of(int e, int E) {
+        const int whole = E / W * W;
+        return FULL || E < W || e < whole ? e : e + W - E % W;
+    }
     __device__ __forceinline__ float at(int p, int w) const { return Type::widen(raw[p][w]); }
 };
 
@@ -322,6 +327,12 @@ __device__ __forceinline__ int id_of(const void* ids, int idx_dtype, int64_t i) 
     return idx_dtype == 1 ? (int)((const uint8_t*)ids)[i] : (int)((const int32_t*)ids)[i];
 }
 
+// v of one lane, the same for all: a scalar
+__device__ __forceinline__ int64_t of_lane(int64_t v, int lane) {
+    const uint32_t low = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane), high = (uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane);
+    return (int64_t)((uint64_t)high << 32 | low);
+}
+
 // How many of the S + 1 ascending offsets are at most t, t the same in all lanes, and the offset after them (INT64_MAX behind the last):
 // 64 probes at a time, so up to 63 sequences take a single load.  Sequence s holds the tokens [off[s], off[s + 1]).
 __device__ __forceinline__ int64_t offsets_up_to(const int64_t* __restrict__ off, int64_t S, int64_t t, int64_t& next) {
@@ -333,7 +344,7 @@ __device__ __forceinline__ int64_t offsets_up_to(const int64_t* __restrict__ off
         const int64_t value = probe < hi ? off[probe] : INT64_MAX;
         const int passed = __popcll(__ballot(value <= t));
         if (passed < 64) {
-            const int64_t above = __shfl(value, passed);
+            const int64_t above = of_lane(value, passed);
             if (above != INT64_MAX) next = above;     // else the one that an earlier round of probes found
         }
         lo += passed * step;
@@ -523,7 +534,7 @@ struct BalanceParts {
 };
 
 constexpr int kPartThreads = 512;
-constexpr int kAloneSequences = 4, kAloneRounds = 4;
+constexpr int kAloneRounds = 4;
 
 struct BalanceOut {
     float alpha;
@@ -548,92 +559,173 @@ __device__ __forceinline__ double wave_sum(double v) {
     return v;
 }
 
-// ALONE: one workgroup takes all tokens and writes the results itself.
+// A chunk is walked in tiles of as many tokens as the workgroup has groups of lanes.  While a tile lies within one sequence, its rows are
+// added up in registers; where a sequence ends, the sums of the lanes are joined through LDS (flush).  Sequences that begin and end
+// inside one tile are added up from a copy of the tile's rows in LDS, each by a wave of its own.
+// ALONE: one workgroup takes all tokens of the only sequence and writes the results itself.
 template <class Type, int L, int V, bool FULL, bool SIGMOID, bool ALONE>
 __global__ __launch_bounds__(kPartThreads) void k_balance_parts(const typename Type::stored* __restrict__ scores, int64_t ld, int64_t T, int E, int k,
                                                                 const uint8_t* __restrict__ token_mask,
                                                                 const void* __restrict__ ids, int idx_dtype,
                                                                 const int64_t* __restrict__ off, int64_t S, BalanceParts parts, BalanceOut out) {
-    constexpr int kWaves = kPartThreads / 64, kTokens = kPartThreads / L;
+    constexpr int kWaves = kPartThreads / 64, kTokens = kPartThreads / L, C = L * V, kAhead = 4, W = kPiece<Type>;
     constexpr int kRows = L <= 16 ? 4 : 64 / L;      // partial sums that a wave leaves in LDS: one per 16 lanes, or per group
-    __shared__ float s_sum[kWaves * kRows][L * V];
-    __shared__ int s_count[L * V];
-    __shared__ int s_tokens;
+    constexpr int kSpan = 64 / kRows;
+    __shared__ float s_rows[kTokens * C];            // a tile's rows, or the waves' partial sums, as the pieces that the lanes hold
+    __shared__ int s_count[C], s_tokens[2];
+    __shared__ int16_t s_ids[kAhead * kPartThreads];  // with a tile's rows, the ids of its first slots
+    __shared__ uint32_t s_few[kWaves][C / 2];        // counts of a sequence inside one tile (at most 8192 slots), two in a word
+    static_assert(kWaves * kRows <= kTokens, "partial sums fit where the rows do");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane % L;
     const int64_t row0 = blockIdx.x * parts.rows, row1 = min(T, row0 + parts.rows);
     if (!ALONE && blockIdx.x == 0 && threadIdx.x == 0) *parts.done = 0;
-    double loss = 0.0;
+    for (int e = threadIdx.x; e < C; e += kPartThreads) s_count[e] = 0;
+    if (threadIdx.x < 2) s_tokens[threadIdx.x] = 0;
     Row<Type, L, V, FULL> x, ahead;
     x.place(part, E);
-    // sequence s is [begin, next); -1 stands for the tokens before the first
-    int64_t s = 0, begin = 0, next = T;
-    if (off && ALONE) {
-        begin = off[0];
-        next = off[1];
-    } else if (off) {
-        s = offsets_up_to(off, S, row0, next) - 1;
-        begin = row0;
-    }
-    for (; s < S; ++s, begin = next, next = off && s < S ? off[s + 1] : T) {
-        if (!ALONE && begin >= row1) break;
-        const int64_t a = max(begin, row0), b = min(next, row1);
-        if (s < 0) continue;
-        if (a >= b) {
-            if (ALONE)
-                for (int e = threadIdx.x; e < E; e += kPartThreads) out.put(s * E + e, E, k, 0, 0.0, 0);
-            continue;
-        }
-        for (int e = threadIdx.x; e < E; e += kPartThreads) s_count[e] = 0;
-        if (threadIdx.x == 0) s_tokens = 0;
-        __syncthreads();
-        float sum[V];
-        int tokens = 0;
+    ahead = x;
+    ahead.load(scores + min(row0 + threadIdx.x / L, row1 - 1) * ld, E);
+    // the walk is in sequence s, whose tokens end before `next`; -1 and S: in none
+    int64_t s = 0, next = T;
+    if (off) s = offsets_up_to(off, S, row0, next) - 1;
+    int64_t window = s + 1, ends = off ? off[min(window + 1 + lane, S)] : 0;     // lane i: the end of sequence window + i
+    double loss = 0.0;
+    bool empty = true, open = false;     // no sequence has been joined yet; the present one has tokens that are not joined
+    float sum[V];
+    int tokens = 0, turn = 0;
 #pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] = 0.f;
-        ahead = x;
-        ahead.load(scores + min(a + threadIdx.x / L, b - 1) * ld, E);
-        const uint32_t slots = (uint32_t)(b - a) * (uint32_t)k;
-#pragma unroll 4
-        for (uint32_t i = threadIdx.x; i < slots; i += kPartThreads) {
-            const int id = id_of(ids, idx_dtype, a * k + i);
-            if ((unsigned)id < (unsigned)E && !(token_mask && token_mask[a + i / (uint32_t)k] == 0)) atomicAdd(&s_count[id], 1);
-        }
-        for (int64_t t0 = a; t0 < b; t0 += kTokens) {
-            const int64_t t = t0 + threadIdx.x / L;
-            x = ahead;
-            const bool live = t < b && !(token_mask && token_mask[t] == 0);
-            tokens += live;
-            if (t0 + kTokens < b) ahead.load(scores + min(t + kTokens, b - 1) * ld, E);
-            float p[V];
-            probabilities<SIGMOID>(x, p);
+    for (int v = 0; v < V; ++v) sum[v] = 0.f;
+    auto emit = [&](int64_t seq, int e, int n, float total, int count) {
+        if (ALONE) loss += out.put(seq * E + e, E, k, n, total, count);
+        else parts.cells[(blockIdx.x + seq) * E + e] = BalanceCell{total, count};
+    };
+    __syncthreads();
+    for (int64_t t0 = row0; t0 < row1; t0 += kTokens) {
+        const int64_t t = t0 + threadIdx.x / L, t1 = min(t0 + kTokens, row1);
+        const bool live = t < row1 && !(token_mask && token_mask[t] == 0);
+        x = ahead;
+        if (t1 < row1) ahead.load(scores + min(t + kTokens, row1 - 1) * ld, E);
+        // the tile's first ids while its probabilities are computed
+        const uint32_t slots = (uint32_t)(t1 - t0) * (uint32_t)k;
+        auto counted = [&](uint32_t i) {
+            const int id = i < slots && !(token_mask && token_mask[t0 + i / (uint32_t)k] == 0) ? id_of(ids, idx_dtype, t0 * k + i) : -1;
+            return (unsigned)id < (unsigned)E ? id : -1;
+        };
+        int id[kAhead];
 #pragma unroll
-            for (int v = 0; v < V; ++v) sum[v] += live ? p[v] : 0.f;
-        }
-        if (part == 0 && tokens) atomicAdd(&s_tokens, tokens);
-        // over the groups within 16 lanes in registers, over the rest in LDS
+        for (int i = 0; i < kAhead; ++i) id[i] = counted(threadIdx.x + i * kPartThreads);
+        float p[V];
+        if (!FULL) {     // compared in every tile: masks that wait for the next one would fill the scalar registers
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            if constexpr (L <= 1) sum[v] += rotated<1>(sum[v]);
-            if constexpr (L <= 2) sum[v] += rotated<2>(sum[v]);
-            if constexpr (L <= 4) sum[v] += rotated<4>(sum[v]);
-            if constexpr (L <= 8) sum[v] += rotated<8>(sum[v]);
-            constexpr int kSpan = 64 / kRows;
-            if (lane % kSpan < L && x.has(v / x.W, v % x.W)) s_sum[wave * kRows + lane / kSpan][x.from[v / x.W] + v % x.W] = sum[v];
+            for (int i = 0; i < x.N; ++i) asm volatile("" : "+v"(x.skip[i]));
         }
-        __syncthreads();
-        const int64_t slot = blockIdx.x + s;
-        for (int e = threadIdx.x; e < E; e += kPartThreads) {
-            float all = 0.f;
+        probabilities<SIGMOID>(x, p);
 #pragma unroll
-            for (int w = 0; w < kWaves * kRows; ++w) all += s_sum[w][e];
-            if (ALONE) loss += out.put(s * E + e, E, k, s_tokens, all, s_count[e]);
-            else parts.cells[slot * E + e] = BalanceCell{all, s_count[e]};
+        for (int v = 0; v < V; ++v) p[v] = live ? p[v] : 0.f;
+        int64_t u = t0;      // the tile's tokens before u are done
+        for (;;) {
+            const int64_t w = min(next, t1);
+            if (s >= 0 && s < S && u < w) {
+                open = true;
+                const bool in = t >= u && t < w;
+#pragma unroll
+                for (int v = 0; v < V; ++v) sum[v] += in ? p[v] : 0.f;
+                tokens += live && in;
+                const uint32_t lo = (uint32_t)(u - t0) * (uint32_t)k, hi = (uint32_t)(w - t0) * (uint32_t)k;
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const uint32_t at = threadIdx.x + i * kPartThreads;
+                    if (id[i] >= 0 && at >= lo && at < hi) atomicAdd(&s_count[id[i]], 1);
+                }
+                for (uint32_t i = threadIdx.x + kAhead * kPartThreads; i < hi; i += kPartThreads) {
+                    const int e = i >= lo ? counted(i) : -1;
+                    if (e >= 0) atomicAdd(&s_count[e], 1);
+                }
+            }
+            if (open && (next < t1 || t1 == row1)) {     // the sequence or the chunk ends
+                open = empty = false;
+                if (part == 0 && tokens) atomicAdd(&s_tokens[turn], tokens);
+                // over the groups within 16 lanes in registers, over the rest in LDS
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    if constexpr (L <= 1) sum[v] += rotated<1>(sum[v]);
+                    if constexpr (L <= 2) sum[v] += rotated<2>(sum[v]);
+                    if constexpr (L <= 4) sum[v] += rotated<4>(sum[v]);
+                    if constexpr (L <= 8) sum[v] += rotated<8>(sum[v]);
+                    if (lane % kSpan < L) s_rows[(wave * kRows + lane / kSpan) * C + (v / W * L + part) * W + v % W] = sum[v];
+                    sum[v] = 0.f;
+                }
+                tokens = 0;
+                __syncthreads();
+                const int n = s_tokens[turn];
+                for (int e = threadIdx.x; e < E; e += kPartThreads) {
+                    float all = 0.f;
+                    const float* rows = s_rows + x.place_of(e, E);
+#pragma unroll 8
+                    for (int w = 0; w < kWaves * kRows; ++w) all += rows[w * C];
+                    emit(s, e, n, all, s_count[e]);
+                    s_count[e] = 0;
+                }
+                if (!ALONE && threadIdx.x == 0) parts.tokens[blockIdx.x + s] = n;
+                turn ^= 1;
+                if (threadIdx.x == 0) s_tokens[turn] = 0;
+                __syncthreads();
+            }
+            if (next >= t1) break;
+            u = max(next, t0);
+            bool copied = false;
+            int whose = 0;
+            for (++s; s < S; ++s) {
+                if (s - window >= 64) {
+                    window = s;
+                    ends = off[min(window + 1 + lane, S)];
+                }
+                next = of_lane(ends, (int)(s - window));
+                if (next >= t1) break;
+                if (next > u) {
+                    empty = false;
+                    if (!copied) {
+                        copied = true;
+#pragma unroll
+                        for (int v = 0; v < V; ++v)
+                            s_rows[threadIdx.x / L * C + (v / W * L + part) * W + v % W] = p[v];
+#pragma unroll
+                        for (int i = 0; i < kAhead; ++i) s_ids[threadIdx.x + i * kPartThreads] = (int16_t)id[i];
+                        __syncthreads();
+                    }
+                    if (whose == wave) {
+                        uint32_t* few = s_few[wave];
+                        for (int e = lane; e < C / 2; e += 64) few[e] = 0;
+                        int n = 0;
+                        const int a = (int)(u - t0), b = (int)(next - t0);
+                        for (int i = a; i < b; i += 64) n += __popcll(__ballot(i + lane < b && !(token_mask && token_mask[t0 + min(i + lane, b - 1)] == 0)));
+                        for (uint32_t i = (uint32_t)a * k + lane; i < (uint32_t)b * k; i += 64) {
+                            const int e = i < kAhead * kPartThreads ? s_ids[i] : counted(i);
+                            if (e >= 0) atomicAdd(&few[e >> 1], 1u << (16 * (e & 1)));
+                        }
+                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                        for (int e = lane; e < E; e += 64) {
+                            float all = 0.f;
+                            const float* rows = s_rows + x.place_of(e, E);
+#pragma unroll 8
+                            for (int i = a; i < b; ++i) all += rows[i * C];
+                            emit(s, e, n, all, (int)(few[e >> 1] >> (16 * (e & 1)) & 0xffffu));
+                        }
+                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                        if (!ALONE && lane == 0) parts.tokens[blockIdx.x + s] = n;
+                    }
+                    whose = whose + 1 == kWaves ? 0 : whose + 1;
+                    u = next;
+                }
+            }
+            if (s >= S) next = INT64_MAX;
+            if (copied) __syncthreads();
         }
-        if (!ALONE && threadIdx.x == 0) parts.tokens[slot] = s_tokens;
-        __syncthreads();
     }
     if (ALONE) {
         __shared__ double s_loss[kWaves];
+        if (empty)
+            for (int e = threadIdx.x; e < E; e += kPartThreads) out.put(e, E, k, 0, 0.0, 0);
         loss = wave_sum(loss);
         if (lane == 0) s_loss[wave] = loss;
         __syncthreads();
@@ -825,7 +917,7 @@ hipError_t launch_balance(const void* scores, int dtype, int64_t ld, int64_t T, 
     const BalanceParts parts{(BalanceCell*)(w + l.cells), (int32_t*)(w + l.tokens), (double*)(w + l.loss), (uint32_t*)(w + l.done), l.rows};
     const BalanceOut out{alpha, counts, prob, coef, loss};
     // one workgroup and no second launch where it needs few rounds: see kAloneRounds
-    const bool alone = S <= kAloneSequences && T <= (int64_t)kAloneRounds * kPartThreads / lanes_of(E);
+    const bool alone = S == 1 && T <= (int64_t)kAloneRounds * kPartThreads / lanes_of(E);
     BalanceParts whole = parts;
     if (alone) whole.rows = T;
     const hipError_t e = with_type(dtype, [&](auto type) {

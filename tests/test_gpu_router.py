@@ -222,6 +222,19 @@ def test_balance_sequences(off, gating):
     check_balance(s, ref, ids, gating, off, mask, with_gates=True)
 
 
+@pytest.mark.parametrize("E,k", [(5, 2), (8, 2), (16, 3), (60, 5), (128, 8), (300, 4), (1000, 3)])
+@pytest.mark.parametrize("n", [3, 40, 300])
+def test_balance_sequences_within_and_across_tiles(E, k, n):
+    """Random cuts, cuts at multiples of 8 (where tiles of tokens end), empty sequences, padding."""
+    T = 700
+    rng = np.random.default_rng(E + n)
+    off = np.sort(np.concatenate([rng.integers(0, T + 1, n), 8 * rng.integers(0, T // 8, n // 2), [128, 256, 512]]))
+    s, ref = make_scores(T, E, torch.bfloat16, n)
+    ids = np.argsort(-ref, axis=1, kind="stable")[:, :k].astype(np.int32)
+    mask = (rng.random(T) < 0.8).astype(np.uint8)
+    check_balance(s, ref, ids, b.GATE_SOFTMAX_ALL if n == 40 else b.GATE_SIGMOID_NORMALISED, off.tolist(), mask)
+
+
 def test_balance_sequences_over_many_chunks():
     """Sequences of 1 to 20000 tokens over the whole grid of chunks, against 64-bit sums of torch."""
     T, E, k = 70001, 64, 6
