@@ -353,32 +353,32 @@ __device__ __forceinline__ int64_t offsets_up_to(const int64_t* __restrict__ off
     return lo;
 }
 
-// Probabilities over all experts of a row, from what a lane holds: softmax, or sigmoids over their sum.  Zero where the lane holds nothing.
+// What the probabilities over all experts of a row are shares of, softmax or sigmoids, from what a lane holds; zero where it holds
+// nothing.  Returns what they are to be multiplied with.  The shift goes into the product with log2 e as a fused sum: its rounding is
+// the same for all of a row, so no share depends on it.
 template <bool SIGMOID, class Type, int L, int V, bool FULL>
-__device__ __forceinline__ void probabilities(const Row<Type, L, V, FULL>& x, float (&prob)[V]) {
+__device__ __forceinline__ float shares(const Row<Type, L, V, FULL>& x, float (&share)[V]) {
     float top = -INFINITY, z = 0.f;
 #pragma unroll
     for (int p = 0; p < x.N; ++p)
 #pragma unroll
         for (int w = 0; w < x.W; ++w) {
-            prob[p * x.W + w] = x.has(p, w) ? x.at(p, w) : -INFINITY;
-            top = fmaxf(top, prob[p * x.W + w]);
+            share[p * x.W + w] = x.has(p, w) ? x.at(p, w) : -INFINITY;
+            top = fmaxf(top, share[p * x.W + w]);
         }
     top = group_max<L>(top);
     if (SIGMOID) {
         top = shift_of(fminf(top, 0.f));
 #pragma unroll
-        for (int v = 0; v < V; ++v) prob[v] = sigmoid_of(prob[v], top);
+        for (int v = 0; v < V; ++v) share[v] = sigmoid_of(share[v], top);
     } else {
-        top = shift_of(top);
+        top = shift_of(top) * 1.44269504f;
 #pragma unroll
-        for (int v = 0; v < V; ++v) prob[v] = exp_of(prob[v] - top);
+        for (int v = 0; v < V; ++v) share[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(share[v], 1.44269504f, -top));
     }
 #pragma unroll
-    for (int v = 0; v < V; ++v) z += prob[v];
-    const float scale = reciprocal_or_zero(group_sum<L>(z));
-#pragma unroll
-    for (int v = 0; v < V; ++v) prob[v] *= scale;
+    for (int v = 0; v < V; ++v) z += share[v];
+    return reciprocal_or_zero(group_sum<L>(z));
 }
 
 struct RouteGrad {
@@ -445,7 +445,8 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
         }
         s = s > a.S ? -1 : s - 1;     // behind the last sequence, as before the first: in none
     }
-    if (WHOLE) probabilities<SIGMOID>(x, prob);
+    float scale = 0.f;
+    if (WHOLE) scale = shares<SIGMOID>(x, prob);
     if (WHOLE && a.coef) {
         float c[V], dot = 0.f;
         const float* coef = a.coef + (s >= 0 ? s : 0) * E;
@@ -455,11 +456,15 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) dot += c[v] * prob[v];
-        dot = group_sum<L>(dot);
+        dot = group_sum<L>(dot) * scale;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            ds[v] = s >= 0 ? prob[v] * (c[v] - dot) : 0.f;
-            if (sigmoid) ds[v] *= s >= 0 ? sigmoid_of(-x.at(v / W, v % W)) : 0.f;
+            ds[v] = prob[v] * scale * (c[v] - dot);
+            if (sigmoid) ds[v] *= sigmoid_of(-x.at(v / W, v % W));
+        }
+        if (__ballot(s < 0)) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) ds[v] = s >= 0 ? ds[v] : 0.f;
         }
     }
     if (a.dlog) {
@@ -481,16 +486,16 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
             top = gate_shift(gating, group_max<L>(top));
             for (int j = part; j < k; j += L)
                 if (e[j] >= 0) z += gate_weight(gating, Type::widen(row[e[j]]), top);
-            const float scale = sum * reciprocal_or_zero(group_sum<L>(z));
+            const float each = sum * reciprocal_or_zero(group_sum<L>(z));
             for (int j = part; j < k; j += L)
-                if (e[j] >= 0) u[j] -= scale * gate_weight(gating, Type::widen(row[e[j]]), top);
+                if (e[j] >= 0) u[j] -= each * gate_weight(gating, Type::widen(row[e[j]]), top);
         }
         if (sigmoid)
             for (int j = part; j < k; j += L)
                 if (e[j] >= 0) u[j] *= sigmoid_of(-Type::widen(row[e[j]]));
         if (WHOLE && gating == kSoftmaxAll) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) ds[v] -= prob[v] * sum;
+            for (int v = 0; v < V; ++v) ds[v] -= prob[v] * (scale * sum);
         }
         __syncthreads();
         for (int j = 0; j < k; ++j) {
@@ -501,9 +506,9 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
         }
     }
     if (!here) return;
-    if (!live) {
+    if (__ballot(!live)) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) ds[v] = 0.f;
+        for (int v = 0; v < V; ++v) ds[v] = live ? ds[v] : 0.f;
     }
 #pragma unroll
     for (int p = 0; p < N; ++p) {
@@ -568,7 +573,8 @@ __global__ __launch_bounds__(kPartThreads) void k_balance_parts(const typename T
                                                                 const uint8_t* __restrict__ token_mask,
                                                                 const void* __restrict__ ids, int idx_dtype,
                                                                 const int64_t* __restrict__ off, int64_t S, BalanceParts parts, BalanceOut out) {
-    constexpr int kWaves = kPartThreads / 64, kTokens = kPartThreads / L, C = L * V, kAhead = 4, W = kPiece<Type>;
+    constexpr int kWaves = kPartThreads / 64, kTokens = kPartThreads / L, C = L * V, W = kPiece<Type>;
+    constexpr int kAhead = L >= 8 ? 1 : L >= 4 ? 2 : 4;      // ids of a tile that a thread fetches ahead: 8 per token, shared by its lanes
     constexpr int kRows = L <= 16 ? 4 : 64 / L;      // partial sums that a wave leaves in LDS: one per 16 lanes, or per group
     constexpr int kSpan = 64 / kRows;
     __shared__ float s_rows[kTokens * C];            // a tile's rows, or the waves' partial sums, as the pieces that the lanes hold
@@ -619,18 +625,27 @@ __global__ __launch_bounds__(kPartThreads) void k_balance_parts(const typename T
 #pragma unroll
             for (int i = 0; i < x.N; ++i) asm volatile("" : "+v"(x.skip[i]));
         }
-        probabilities<SIGMOID>(x, p);
+        float scale = shares<SIGMOID>(x, p);
+        if (__ballot(!live)) {     // (what a padding token holds may be NaN)
+            scale = live ? scale : 0.f;
 #pragma unroll
-        for (int v = 0; v < V; ++v) p[v] = live ? p[v] : 0.f;
+            for (int v = 0; v < V; ++v) p[v] = live ? p[v] : 0.f;
+        }
         int64_t u = t0;      // the tile's tokens before u are done
         for (;;) {
             const int64_t w = min(next, t1);
             if (s >= 0 && s < S && u < w) {
                 open = true;
-                const bool in = t >= u && t < w;
+                const bool in = live && t >= u && t < w;
+                const float take = in ? scale : 0.f;
+                if ((u == t0 && w == t1) || __ballot(in) == ~0ull) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) sum[v] += in ? p[v] : 0.f;
-                tokens += live && in;
+                    for (int v = 0; v < V; ++v) sum[v] = __builtin_fmaf(p[v], take, sum[v]);
+                } else {     // another sequence's NaN stays its own
+#pragma unroll
+                    for (int v = 0; v < V; ++v) sum[v] += in ? p[v] * scale : 0.f;
+                }
+                tokens += in;
                 const uint32_t lo = (uint32_t)(u - t0) * (uint32_t)k, hi = (uint32_t)(w - t0) * (uint32_t)k;
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) {
@@ -688,7 +703,7 @@ __global__ __launch_bounds__(kPartThreads) void k_balance_parts(const typename T
                         copied = true;
 #pragma unroll
                         for (int v = 0; v < V; ++v)
-                            s_rows[threadIdx.x / L * C + (v / W * L + part) * W + v % W] = p[v];
+                            s_rows[threadIdx.x / L * C + (v / W * L + part) * W + v % W] = p[v] * scale;
 #pragma unroll
                         for (int i = 0; i < kAhead; ++i) s_ids[threadIdx.x + i * kPartThreads] = (int16_t)id[i];
                         __syncthreads();
