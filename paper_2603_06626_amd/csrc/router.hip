@@ -538,7 +538,7 @@ struct BalanceParts {
     int64_t rows;        // of a chunk
 };
 
-constexpr int kPartThreads = 512;
+constexpr int kPartThreads = 256;
 constexpr int kAloneRounds = 4;
 
 struct BalanceOut {
@@ -580,7 +580,7 @@ __global__ __launch_bounds__(kPartThreads) void k_balance_parts(const typename T
     __shared__ float s_rows[kTokens * C];            // a tile's rows, or the waves' partial sums, as the pieces that the lanes hold
     __shared__ int s_count[C], s_tokens[2];
     __shared__ int16_t s_ids[kAhead * kPartThreads];  // with a tile's rows, the ids of its first slots
-    __shared__ uint32_t s_few[kWaves][C / 2];        // counts of a sequence inside one tile (at most 8192 slots), two in a word
+    __shared__ uint32_t s_few[kWaves][C / 2];        // counts of a sequence inside one tile (at most 4096 slots), two in a word
     static_assert(kWaves * kRows <= kTokens, "partial sums fit where the rows do");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane % L;
     const int64_t row0 = blockIdx.x * parts.rows, row1 = min(T, row0 + parts.rows);
