@@ -15,18 +15,25 @@
 // formulas alone.
 #include "lanes.hpp"
 
+#include <type_traits>
+
 #pragma clang fp contract(off)
 
 namespace grouter {
 
 namespace {
 
-constexpr int kThreads = 256, kEach = 8;              // elements of a thread: 16 bytes of bf16, a quarter of a block of moments
+constexpr int kThreads = 256;
 constexpr int kBlock = 32;                            // elements under one exponent
-constexpr int kPasses = 4;
-constexpr int64_t kPerGroup = kThreads * kEach * kPasses;
 
 enum ParamKind { kFp32Param = 0, kMasterParam = 1, kBf16Param = 2 };
+
+// Elements of a thread: 4, which are 16 bytes of every fp32 stream, so that a wave's loads are whole lines one after the other; 8 where no
+// stream is that wide.  Measured on 12 bf16 tensors of 262144 with fp32 masters and moments, 75 fp32 ones of up to 300001 with 8-bit
+// moments, 554 M elements of the former kind and as many in bf16 with 8-bit moments: 4 elements 15.2, 41.2, 2880, 1230 us, 8 elements
+// 16.6, 45.4, 2977, 1150, 16 elements 22.1, 59.0, 3477, 1138.  One such piece per thread and no loop: two to eight in a row took 1.1 times
+// as long.
+constexpr int each_of(int kind, bool grad_bf16, bool eight) { return kind == kBf16Param && grad_bf16 && eight ? 8 : 4; }
 
 struct Batch {
     AdamwTensor tensor[kAdamwPerLaunch];
@@ -72,28 +79,132 @@ __device__ __forceinline__ void decode4(uint32_t codes, float scale, float* out)
     out[3] = b.y * scale;
 }
 
-// kEach elements from p on, n of them there, the others 0
-template <class Type>
-__device__ __forceinline__ void fetch(const void* p, int64_t at, int n, float* out) {
+constexpr int min_of(int a, int b) { return a < b ? a : b; }
+
+// kEach elements from place `at` on; not WHOLE: n of them there, the others 0
+template <class Type, int kEach, bool WHOLE>
+__device__ __forceinline__ void fetch(const void* p, int64_t at, int n, typename Type::stored* out) {
     const auto* q = (const typename Type::stored*)p + at;
-    if (n == kEach) {
-        typename Type::stored raw[kEach];
-        __builtin_memcpy(raw, __builtin_assume_aligned(q, 16), sizeof(raw));
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) out[i] = Type::widen(raw[i]);
+    if (WHOLE) {
+        __builtin_memcpy(out, __builtin_assume_aligned(q, min_of(16, kEach * (int)sizeof(*q))), kEach * sizeof(*q));
     } else {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) out[i] = i < n ? Type::widen(q[i]) : 0.f;
+        for (int i = 0; i < kEach; ++i) out[i] = i < n ? q[i] : typename Type::stored(0);
     }
 }
-template <class T>
+template <int kEach, bool WHOLE, class T>
 __device__ __forceinline__ void put(T* p, int64_t at, int n, const T* v) {
-    if (n == kEach) {
-        __builtin_memcpy(__builtin_assume_aligned(p + at, sizeof(T) == 1 ? 8 : 16), v, sizeof(T) * kEach);
+    if (WHOLE) {
+        __builtin_memcpy(__builtin_assume_aligned(p + at, min_of(16, kEach * (int)sizeof(T))), v, sizeof(T) * kEach);
     } else {
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
             if (i < n) p[at + i] = v[i];
+    }
+}
+struct Byte {
+    typedef uint8_t stored;
+};
+
+// The step of kEach elements.  WHOLE: the workgroup's elements all exist, so that every stream is one or two loads without a branch,
+// all on their way before the first is waited for (a choice per stream between whole and single loads had the compiler wait after each).
+template <int KIND, class Grad, bool EIGHT, bool WHOLE>
+__device__ __forceinline__ void step(const AdamwTensor& t, const AdamwHyper& h, float scale, uint64_t place, int64_t at, int n) {
+    constexpr int kEach = each_of(KIND, std::is_same_v<Grad, Bf16>, EIGHT);
+    typedef std::conditional_t<KIND == kBf16Param, Bf16, Fp32> Weight;
+    typedef std::conditional_t<EIGHT, Byte, Fp32> Moment;
+    typename Grad::stored raw_g[kEach];
+    typename Weight::stored raw_w[kEach];
+    typename Moment::stored raw_m[kEach], raw_v[kEach];
+    const int64_t from = WHOLE || n > 0 ? at : 0;
+    fetch<Grad, kEach, WHOLE>(t.grad, from, n, raw_g);
+    fetch<Weight, kEach, WHOLE>(KIND == kMasterParam ? t.master : t.param, from, n, raw_w);
+    fetch<Moment, kEach, WHOLE>(t.m, from, n, raw_m);
+    fetch<Moment, kEach, WHOLE>(t.v, from, n, raw_v);
+    float m[kEach], v[kEach], w[kEach];
+    if constexpr (EIGHT) {
+        const float sm = power_of_two(t.m_exp[from / kBlock]), sv = power_of_two(t.v_exp[from / kBlock]);
+#pragma unroll
+        for (int j = 0; j < kEach; j += 4) {
+            uint32_t a, b;
+            __builtin_memcpy(&a, raw_m + j, 4);
+            __builtin_memcpy(&b, raw_v + j, 4);
+            decode4(a, sm, m + j);
+            decode4(b, sv, v + j);
+        }
+        if (!WHOLE) {     // zero times a block that is NaN
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                m[j] = j < n ? m[j] : 0.f;
+                v[j] = j < n ? v[j] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) v[j] = v[j] * v[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            m[j] = raw_m[j];
+            v[j] = raw_v[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const float s = Grad::widen(raw_g[j]) * scale;
+        w[j] = Weight::widen(raw_w[j]);
+        m[j] = m[j] * h.beta1 + s * h.one_minus_beta1;
+        v[j] = v[j] * h.beta2 + s * s * h.one_minus_beta2;
+        w[j] = w[j] - (w[j] * h.decay + m[j] * __builtin_amdgcn_rcpf(root_of(v[j]) * h.inv_root_correction + h.eps) * h.step_size);
+    }
+    uint32_t noise[kEach];
+    if (EIGHT || KIND == kBf16Param) {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) noise[j] = noise_of(place + at + j, h.seed);
+    }
+    if (KIND == kFp32Param) put<kEach, WHOLE>((float*)t.param, at, n, w);
+    if (KIND == kMasterParam) put<kEach, WHOLE>(t.master, at, n, w);
+    if (KIND != kFp32Param) {
+        uint16_t b[kEach];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            b[j] = Bf16::narrow(w[j]);
+            if (KIND == kBf16Param) {   // a step is often less than half a unit of bf16: up or down with the probability of the remainder
+                const uint32_t u = __float_as_uint(w[j]);
+                b[j] = (u & 0x7fffffffu) < 0x7f800000u ? (uint16_t)((u + (noise[j] >> 16)) >> 16) : b[j];
+            }
+        }
+        put<kEach, WHOLE>((uint16_t*)t.param, at, n, b);
+    }
+    if (!EIGHT) {
+        put<kEach, WHOLE>((float*)t.m, at, n, m);
+        put<kEach, WHOLE>((float*)t.v, at, n, v);
+    } else {
+        uint32_t pm = 0, pv = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            if (!WHOLE && j >= n) m[j] = v[j] = 0.f;     // (a scale that is not finite makes NaN of no gradient, too)
+            pm = max(pm, __float_as_uint(m[j]) & 0x7fffffffu);
+            pv = max(pv, __float_as_uint(v[j]));
+        }
+        pm = group_max<kBlock / kEach>(pm);
+        pv = group_max<kBlock / kEach>(pv);
+        // the least power of two under which the largest is at most 448 = 1.75 * 2^8; for the root of v, 1.75^2 = 3.0625 per 4^k
+        const int em = pm >= 0x7f800000u ? 255 : max((int)((pm + 0x1fffffu) >> 23) - 8, 0);
+        // (numbers below 2^-126 have no leading bit to go by: 56 fits them all)
+        const int ev = pv >= 0x7f800000u ? 255 : pv - 1u < 0x7fffffu ? 56 : (((int)pv - (127 << 23) + 0x3bffff) >> 24) + 119;
+        uint8_t cm[kEach], cv[kEach];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            cm[j] = (uint8_t)(code_of(fabsf(m[j]), em, noise[j] >> 12) | (__float_as_uint(m[j]) >> 31 << 7));
+            const uint32_t c = code_of(root_of(v[j]), ev, (noise[j] & 0xfffu) << 8 | 128u);
+            cv[j] = (uint8_t)(v[j] > 0.f ? max(c, 1u) : c);
+        }
+        put<kEach, WHOLE>((uint8_t*)t.m, at, n, cm);
+        put<kEach, WHOLE>((uint8_t*)t.v, at, n, cv);
+        if ((WHOLE || n > 0) && at % kBlock == 0) {
+            t.m_exp[at / kBlock] = (uint8_t)em;
+            t.v_exp[at / kBlock] = (uint8_t)ev;
+        }
     }
 }
 
@@ -105,98 +216,11 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const Batch batch) {
     const AdamwTensor t = batch.tensor[i];
     const AdamwHyper h = batch.hyper_device ? *batch.hyper_device : batch.hyper;
     const float scale = batch.grad_scale ? h.grad_scale * *batch.grad_scale : h.grad_scale;
-    const int64_t begin = (int64_t)(blockIdx.x - batch.first_group[i]) * kPerGroup;
-#pragma unroll
-    for (int pass = 0; pass < kPasses; ++pass) {
-        const int64_t at = begin + ((int64_t)pass * kThreads + threadIdx.x) * kEach;
-        const int n = (int)max((int64_t)0, min((int64_t)kEach, t.n - at));
-        if (__ballot(n > 0) == 0) return;
-        float g[kEach], m[kEach], v[kEach], w[kEach];
-        fetch<Grad>(t.grad, n ? at : 0, n, g);
-        if (KIND == kBf16Param) fetch<Bf16>(t.param, n ? at : 0, n, w);
-        else fetch<Fp32>(KIND == kMasterParam ? t.master : t.param, n ? at : 0, n, w);
-        if (EIGHT) {
-            uint32_t cm[2] = {0, 0}, cv[2] = {0, 0};
-            const auto* qm = (const uint8_t*)t.m + at;
-            const auto* qv = (const uint8_t*)t.v + at;
-            if (n == kEach) {
-                __builtin_memcpy(cm, __builtin_assume_aligned(qm, 8), 8);
-                __builtin_memcpy(cv, __builtin_assume_aligned(qv, 8), 8);
-            } else {
-                for (int j = 0; j < n; ++j) {
-                    cm[j / 4] |= (uint32_t)qm[j] << (8 * (j & 3));
-                    cv[j / 4] |= (uint32_t)qv[j] << (8 * (j & 3));
-                }
-            }
-            const float sm = power_of_two(n ? t.m_exp[at / kBlock] : 0), sv = power_of_two(n ? t.v_exp[at / kBlock] : 0);
-            decode4(cm[0], sm, m);
-            decode4(cm[1], sm, m + 4);
-            decode4(cv[0], sv, v);
-            decode4(cv[1], sv, v + 4);
-#pragma unroll
-            for (int j = 0; j < kEach; ++j) v[j] = v[j] * v[j];
-        } else {
-            fetch<Fp32>(t.m, n ? at : 0, n, m);
-            fetch<Fp32>(t.v, n ? at : 0, n, v);
-        }
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-            const float s = g[j] * scale;
-            m[j] = m[j] * h.beta1 + s * h.one_minus_beta1;
-            v[j] = v[j] * h.beta2 + s * s * h.one_minus_beta2;
-            w[j] = w[j] - (w[j] * h.decay + m[j] * __builtin_amdgcn_rcpf(root_of(v[j]) * h.inv_root_correction + h.eps) * h.step_size);
-        }
-        uint32_t noise[kEach];
-        if (EIGHT || KIND == kBf16Param) {
-            const uint64_t place = batch.first_place[i] + at;
-#pragma unroll
-            for (int j = 0; j < kEach; ++j) noise[j] = noise_of(place + j, h.seed);
-        }
-        if (KIND == kFp32Param) put((float*)t.param, at, n, w);
-        if (KIND == kMasterParam) put(t.master, at, n, w);
-        if (KIND != kFp32Param) {
-            uint16_t b[kEach];
-#pragma unroll
-            for (int j = 0; j < kEach; ++j) {
-                b[j] = Bf16::narrow(w[j]);
-                if (KIND == kBf16Param) {   // a step is often less than half a unit of bf16: up or down with the probability of the remainder
-                    const uint32_t u = __float_as_uint(w[j]);
-                    b[j] = (u & 0x7fffffffu) < 0x7f800000u ? (uint16_t)((u + (noise[j] >> 16)) >> 16) : b[j];
-                }
-            }
-            put((uint16_t*)t.param, at, n, b);
-        }
-        if (!EIGHT) {
-            put((float*)t.m, at, n, m);
-            put((float*)t.v, at, n, v);
-        } else {
-            uint32_t pm = 0, pv = 0;
-#pragma unroll
-            for (int j = 0; j < kEach; ++j) {
-                pm = max(pm, __float_as_uint(m[j]) & 0x7fffffffu);
-                pv = max(pv, __float_as_uint(v[j]));
-            }
-            pm = group_max<kBlock / kEach>(pm);
-            pv = group_max<kBlock / kEach>(pv);
-            // the least power of two under which the largest is at most 448 = 1.75 * 2^8; for the root of v, 1.75^2 = 3.0625 per 4^k
-            const int em = pm >= 0x7f800000u ? 255 : max((int)((pm + 0x1fffffu) >> 23) - 8, 0);
-            // (numbers below 2^-126 have no leading bit to go by: 56 fits them all)
-            const int ev = pv >= 0x7f800000u ? 255 : pv - 1u < 0x7fffffu ? 56 : (((int)pv - (127 << 23) + 0x3bffff) >> 24) + 119;
-            uint8_t cm[kEach], cv[kEach];
-#pragma unroll
-            for (int j = 0; j < kEach; ++j) {
-                cm[j] = (uint8_t)(code_of(fabsf(m[j]), em, noise[j] >> 12) | (__float_as_uint(m[j]) >> 31 << 7));
-                const uint32_t c = code_of(root_of(v[j]), ev, (noise[j] & 0xfffu) << 8 | 128u);
-                cv[j] = (uint8_t)(v[j] > 0.f ? max(c, 1u) : c);
-            }
-            put((uint8_t*)t.m, at, n, cm);
-            put((uint8_t*)t.v, at, n, cv);
-            if (n > 0 && at % kBlock == 0) {
-                t.m_exp[at / kBlock] = (uint8_t)em;
-                t.v_exp[at / kBlock] = (uint8_t)ev;
-            }
-        }
-    }
+    constexpr int kEach = each_of(KIND, std::is_same_v<Grad, Bf16>, EIGHT);
+    constexpr int64_t kPerGroup = kThreads * kEach;
+    const int64_t begin = (int64_t)(blockIdx.x - batch.first_group[i]) * kPerGroup, at = begin + (int64_t)threadIdx.x * kEach;
+    if (begin + kPerGroup <= t.n) step<KIND, Grad, EIGHT, true>(t, h, scale, batch.first_place[i], at, kEach);
+    else step<KIND, Grad, EIGHT, false>(t, h, scale, batch.first_place[i], at, (int)max((int64_t)0, min((int64_t)kEach, t.n - at)));
 }
 
 template <int KIND, class Grad, bool EIGHT>
@@ -227,6 +251,7 @@ hipError_t launch_adamw(const AdamwTensor* tensors, int count, int param_kind, i
     if (host) b.hyper = *host;
     b.hyper_device = device;
     b.grad_scale = grad_scale;
+    const uint64_t per_group = (uint64_t)kThreads * each_of(param_kind, grad_dtype == 1, state_bits == 8);
     uint64_t place = 0;
     uint64_t groups = 0;
     auto flush = [&]() {
@@ -237,7 +262,7 @@ hipError_t launch_adamw(const AdamwTensor* tensors, int count, int param_kind, i
         return e;
     };
     for (int i = 0; i < count; ++i) {
-        const uint64_t need = ((uint64_t)tensors[i].n + kPerGroup - 1) / kPerGroup;
+        const uint64_t need = ((uint64_t)tensors[i].n + per_group - 1) / per_group;
         if (tensors[i].n > 0) {
             if (b.count == kAdamwPerLaunch || groups + need > 0x7fffffffu) {
                 const hipError_t e = flush();
