@@ -46,8 +46,12 @@ struct Batch {
 };
 static_assert(sizeof(Batch) <= 4000, "a launch's arguments are limited to 4 KB");
 
-__device__ __forceinline__ uint32_t noise_of(uint64_t place, uint32_t seed) {
-    uint32_t h = (uint32_t)place + (uint32_t)(place >> 32) * 0x632BE5ABu + seed * 0x9E3779B1u;
+// 32 random bits of an element, from its place in the list and the seed: noise_of(first_noise(place, seed) + j) for the j-th behind one
+// whose place is a multiple of 4 or 8, j below that
+__device__ __forceinline__ uint32_t first_noise(uint64_t place, uint32_t seed) {
+    return (uint32_t)place + (uint32_t)(place >> 32) * 0x632BE5ABu + seed * 0x9E3779B1u;
+}
+__device__ __forceinline__ uint32_t noise_of(uint32_t h) {
     h ^= h >> 16;
     h *= 0xA3D95FA9u;
     h ^= h >> 15;
@@ -55,10 +59,22 @@ __device__ __forceinline__ uint32_t noise_of(uint64_t place, uint32_t seed) {
     return h ^ (h >> 16);
 }
 
-// sqrt(v) to 1 unit; the hardware's takes what is below 2^-126 for 0
-__device__ __forceinline__ float root_of(float v) {
-    const bool small = v < 0x1p-96f;
-    return __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v) * (small ? 0x1p-32f : 1.f);
+// sqrt(v) to 1 unit; the hardware's takes what is below 2^-126 for 0, so where a wave holds such numbers (zeros mostly) all go the longer way
+template <int N>
+__device__ __forceinline__ void roots_of(const float (&v)[N], float (&root)[N]) {
+    float least = v[0];
+#pragma unroll
+    for (int j = 1; j < N; ++j) least = fminf(least, v[j]);
+    if (__ballot(least < 0x1p-96f)) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const bool small = v[j] < 0x1p-96f;
+            root[j] = __builtin_amdgcn_sqrtf(small ? v[j] * 0x1p64f : v[j]) * (small ? 0x1p-32f : 1.f);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) root[j] = __builtin_amdgcn_sqrtf(v[j]);
+    }
 }
 __device__ __forceinline__ float power_of_two(int biased) {   // 2^(biased - 127); 255 is NaN
     return __uint_as_float(biased == 255 ? 0x7fc00000u : biased == 0 ? 0x00400000u : (uint32_t)biased << 23);
@@ -121,7 +137,7 @@ __device__ __forceinline__ void step(const AdamwTensor& t, const AdamwHyper& h, 
     fetch<Weight, kEach, WHOLE>(KIND == kMasterParam ? t.master : t.param, from, n, raw_w);
     fetch<Moment, kEach, WHOLE>(t.m, from, n, raw_m);
     fetch<Moment, kEach, WHOLE>(t.v, from, n, raw_v);
-    float m[kEach], v[kEach], w[kEach];
+    float m[kEach], v[kEach], w[kEach], root[kEach];
     if constexpr (EIGHT) {
         const float sm = power_of_two(t.m_exp[from / kBlock]), sv = power_of_two(t.v_exp[from / kBlock]);
 #pragma unroll
@@ -154,12 +170,16 @@ __device__ __forceinline__ void step(const AdamwTensor& t, const AdamwHyper& h, 
         w[j] = Weight::widen(raw_w[j]);
         m[j] = m[j] * h.beta1 + s * h.one_minus_beta1;
         v[j] = v[j] * h.beta2 + s * s * h.one_minus_beta2;
-        w[j] = w[j] - (w[j] * h.decay + m[j] * __builtin_amdgcn_rcpf(root_of(v[j]) * h.inv_root_correction + h.eps) * h.step_size);
     }
+    roots_of(v, root);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+        w[j] = w[j] - (w[j] * h.decay + m[j] * __builtin_amdgcn_rcpf(root[j] * h.inv_root_correction + h.eps) * h.step_size);
     uint32_t noise[kEach];
     if (EIGHT || KIND == kBf16Param) {
+        const uint32_t first = first_noise(place + at, h.seed);
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) noise[j] = noise_of(place + at + j, h.seed);
+        for (int j = 0; j < kEach; ++j) noise[j] = noise_of(first + j);
     }
     if (KIND == kFp32Param) put<kEach, WHOLE>((float*)t.param, at, n, w);
     if (KIND == kMasterParam) put<kEach, WHOLE>(t.master, at, n, w);
@@ -182,7 +202,7 @@ __device__ __forceinline__ void step(const AdamwTensor& t, const AdamwHyper& h, 
         uint32_t pm = 0, pv = 0;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            if (!WHOLE && j >= n) m[j] = v[j] = 0.f;     // (a scale that is not finite makes NaN of no gradient, too)
+            if (!WHOLE && j >= n) m[j] = v[j] = root[j] = 0.f;     // (a scale that is not finite makes NaN of no gradient, too)
             pm = max(pm, __float_as_uint(m[j]) & 0x7fffffffu);
             pv = max(pv, __float_as_uint(v[j]));
         }
@@ -196,7 +216,7 @@ __device__ __forceinline__ void step(const AdamwTensor& t, const AdamwHyper& h, 
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             cm[j] = (uint8_t)(code_of(fabsf(m[j]), em, noise[j] >> 12) | (__float_as_uint(m[j]) >> 31 << 7));
-            const uint32_t c = code_of(root_of(v[j]), ev, (noise[j] & 0xfffu) << 8 | 128u);
+            const uint32_t c = code_of(root[j], ev, (noise[j] & 0xfffu) << 8 | 128u);
             cv[j] = (uint8_t)(v[j] > 0.f ? max(c, 1u) : c);
         }
         put<kEach, WHOLE>((uint8_t*)t.m, at, n, cm);
