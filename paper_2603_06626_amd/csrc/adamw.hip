@@ -79,12 +79,25 @@ __device__ __forceinline__ void roots_of(const float (&v)[N], float (&root)[N]) 
 __device__ __forceinline__ float power_of_two(int biased) {   // 2^(biased - 127); 255 is NaN
     return __uint_as_float(biased == 255 ? 0x7fc00000u : biased == 0 ? 0x00400000u : (uint32_t)biased << 23);
 }
-// e4m3 code of x >= 0 times 2^(127 - exp); up: 20 random bits
-__device__ __forceinline__ uint32_t code_of(float x, int exp, uint32_t up) {
-    const float y = x * power_of_two(254 - exp);
-    const uint32_t normal = ((__float_as_uint(y) + up) >> 20) - 960u;
-    const uint32_t small = (uint32_t)(y * 512.f + (float)up * 0x1p-20f);
-    return exp == 255 ? 127u : min(y < 0x1p-6f ? small : normal, 126u);
+// e4m3 codes of x >= 0 times 2^(127 - exp); up: 20 random bits each.  Numbers below 2^-6 (less than a 28000th of the block's largest) have
+// codes in equal steps, and blocks that are not finite one code for all: both are looked at only where a wave has some.
+template <int N>
+__device__ __forceinline__ void codes_of(const float (&x)[N], int exp, const uint32_t (&up)[N], uint32_t (&code)[N]) {
+    const float scale = power_of_two(254 - exp);
+    float y[N], least = INFINITY;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        y[j] = x[j] * scale;
+        least = fminf(least, y[j]);
+        code[j] = min(((__float_as_uint(y[j]) + up[j]) >> 20) - 960u, 126u);
+    }
+    if (__ballot(least < 0x1p-6f || exp == 255)) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const uint32_t small = (uint32_t)(y[j] * 512.f + (float)up[j] * 0x1p-20f);
+            code[j] = exp == 255 ? 127u : y[j] < 0x1p-6f ? small : code[j];
+        }
+    }
 }
 __device__ __forceinline__ void decode4(uint32_t codes, float scale, float* out) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -212,13 +225,23 @@ __device__ __forceinline__ void step(const AdamwTensor& t, const AdamwHyper& h, 
         const int em = pm >= 0x7f800000u ? 255 : max((int)((pm + 0x1fffffu) >> 23) - 8, 0);
         // (numbers below 2^-126 have no leading bit to go by: 56 fits them all)
         const int ev = pv >= 0x7f800000u ? 255 : pv - 1u < 0x7fffffu ? 56 : (((int)pv - (127 << 23) + 0x3bffff) >> 24) + 119;
+        uint32_t up[kEach], code[kEach];
+        float size[kEach];
         uint8_t cm[kEach], cv[kEach];
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            cm[j] = (uint8_t)(code_of(fabsf(m[j]), em, noise[j] >> 12) | (__float_as_uint(m[j]) >> 31 << 7));
-            const uint32_t c = code_of(root[j], ev, (noise[j] & 0xfffu) << 8 | 128u);
-            cv[j] = (uint8_t)(v[j] > 0.f ? max(c, 1u) : c);
+            size[j] = fabsf(m[j]);
+            up[j] = noise[j] >> 12;
         }
+        codes_of(size, em, up, code);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            cm[j] = (uint8_t)(code[j] | (__float_as_uint(m[j]) >> 31 << 7));
+            up[j] = (noise[j] & 0xfffu) << 8 | 128u;
+        }
+        codes_of(root, ev, up, code);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) cv[j] = (uint8_t)(v[j] > 0.f ? max(code[j], 1u) : code[j]);
         put<kEach, WHOLE>((uint8_t*)t.m, at, n, cm);
         put<kEach, WHOLE>((uint8_t*)t.v, at, n, cv);
         if ((WHOLE || n > 0) && at % kBlock == 0) {
