@@ -23,7 +23,7 @@
  *   Every pointer is a DEVICE pointer owned by the caller unless stated otherwise; the library never
  *   allocates or frees device memory.  `stream` is a hipStream_t passed as void* (NULL = default
  *   stream).  Calls only enqueue work and return; the single exception is grouter_plan_status.
- *   Outputs are overwritten in full, never accumulated into.
+ *   Outputs are overwritten in full, never accumulated into (grouter_adamw updates its tensors in place).
  *   Limits: 1 <= k <= E <= 1024 (E <= 256 for uint8 ids), T*k < 2^31, d % 8 == 0, f % 8 == 0,
  *   d*f*2 < 2^31 (one expert's weight slab) and T*k*max(d,f)*2 < 2^31 (an activation matrix in
  *   expert-sorted order): the kernels use 32-bit byte offsets inside those.  The size queries return
@@ -227,7 +227,9 @@ int grouter_fold_weights(const float* W_s, const int32_t* group_of, int d, int E
  * Scores are a matrix [T][E] of fp32, bf16 or fp16 (GROUTER_FP32 ...) whose rows are score_ld >= E elements apart, so it
  * may be part of a wider one; only its own elements are read.  Rows that start at multiples of 16 bytes are read faster.
  * token_mask [T] uint8 or NULL: tokens with 0 are padding and their scores may hold anything.
- * Limits: 1 <= k <= E <= 1024 (E <= 256 for uint8 ids), T*k < 2^31, 1 <= S <= 2^24; no two arguments may overlap.
+ * Limits: 1 <= k <= E <= 1024 (E <= 256 for uint8 ids), T*k < 2^31, score_ld <= 2^31, T*score_ld <= 2^48, 1 <= S <= 2^24.  No output may
+ * overlap another argument (two matrices may be different columns of one).  Calls that may overlap in time need outputs and
+ * workspaces of their own; that holds for captured graphs that replay side by side, too.
  */
 
 /* How gates come from scores (Eq. 2, r = g(TopK(s, k))): g a softmax over the k selected scores, the selected ones' shares

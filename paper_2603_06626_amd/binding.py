@@ -160,6 +160,16 @@ def _stream(stream=None):
     return _raw_stream()
 
 
+def _stream_for(t, stream=None):
+    """The stream to enqueue on: the given one, or the current one of the current device, which has to be the one that t is on."""
+    import torch
+
+    device = torch.cuda.current_device() if stream is None else stream.device.index
+    if t.get_device() != device:
+        raise ValueError(f"the tensors are on device {t.get_device()}, the stream is device {device}'s")
+    return _stream(stream)
+
+
 def _dev(t, name, dtype=None):
     if not (t.is_cuda and t.is_contiguous()):
         raise ValueError(f"{name} must be a contiguous GPU tensor")
@@ -487,7 +497,7 @@ def grouter_route(scores, k, gating, topk_idx, gate_w, token_mask=None, stream=N
     if topk_idx.shape != (T, k) or gate_w.shape != (T, k):
         raise ValueError("shape mismatch")
     _check(lib().grouter_route(_p(scores), _float_dtype(scores, "scores"), ld, T, E, k, gating, _mask(token_mask, T), _p(topk_idx),
-                               _idx_dtype(topk_idx), _p(gate_w), _stream(stream)), "grouter_route")
+                               _idx_dtype(topk_idx), _p(gate_w), _stream_for(scores, stream)), "grouter_route")
 
 
 def grouter_route_bwd(scores, gating, dscores, topk_idx=None, dlog_gate=None, token_mask=None, seq_offsets=None, coef=None, stream=None):
@@ -508,7 +518,7 @@ def grouter_route_bwd(scores, gating, dscores, topk_idx=None, dlog_gate=None, to
         raise ValueError("shape mismatch")
     _check(lib().grouter_route_bwd(_p(scores), _float_dtype(scores, "scores"), ld, T, E, gating, _mask(token_mask, T),
                                    _p(topk_idx) if k else None, it, k, _p(dlog_gate), off, S, _p(coef), _p(dscores),
-                                   _float_dtype(dscores, "dscores"), dld, _stream(stream)), "grouter_route_bwd")
+                                   _float_dtype(dscores, "dscores"), dld, _stream_for(scores, stream)), "grouter_route_bwd")
 
 
 def grouter_balance_bytes(T, E, S) -> int:
@@ -531,7 +541,7 @@ def grouter_balance(scores, gating, topk_idx, alpha, counts, prob, coef, loss, w
         raise ValueError("shape mismatch")
     _check(lib().grouter_balance(_p(scores), _float_dtype(scores, "scores"), ld, T, E, k, gating, _mask(token_mask, T), _p(topk_idx),
                                  _idx_dtype(topk_idx), off, S, alpha, _p(counts), _p(prob), _p(coef), _p(loss), _p(_dev(ws, "ws")),
-                                 ws.numel() * ws.element_size(), _stream(stream)), "grouter_balance")
+                                 ws.numel() * ws.element_size(), _stream_for(scores, stream)), "grouter_balance")
 
 
 def grouter_gate_bwd(plan_ws, T, k, E, dY, inp, dlog_gate, stream=None):
@@ -545,7 +555,7 @@ def grouter_gate_bwd(plan_ws, T, k, E, dY, inp, dlog_gate, stream=None):
     d = dY.shape[1]
     if dY.shape != (T, d) or inp.shape != (T * k, d) or dlog_gate.shape != (T, k) or plan_ws.numel() < grouter_plan_bytes(T, k, E):
         raise ValueError("shape mismatch")
-    _check(lib().grouter_gate_bwd(_p(plan_ws), T, k, E, d, _p(dY), _p(inp), _p(dlog_gate), _stream(stream)), "grouter_gate_bwd")
+    _check(lib().grouter_gate_bwd(_p(plan_ws), T, k, E, d, _p(dY), _p(inp), _p(dlog_gate), _stream_for(dY, stream)), "grouter_gate_bwd")
 
 
 def grouter_moe_gate_bwd(plan_ws, E, f, dY, ctx_ws, dlog_gate, stream=None):
@@ -560,7 +570,7 @@ def grouter_moe_gate_bwd(plan_ws, E, f, dY, ctx_ws, dlog_gate, stream=None):
     d = dY.shape[1]
     if dY.shape != (T, d) or plan_ws.numel() < grouter_plan_bytes(T, k, E):
         raise ValueError("shape mismatch")
-    _check(lib().grouter_moe_gate_bwd(_p(plan_ws), T, k, E, d, f, _p(dY), _p(ctx_ws), ctx_ws.numel(), _p(dlog_gate), _stream(stream)),
+    _check(lib().grouter_moe_gate_bwd(_p(plan_ws), T, k, E, d, f, _p(dY), _p(ctx_ws), ctx_ws.numel(), _p(dlog_gate), _stream_for(dY, stream)),
            "grouter_moe_gate_bwd")
 
 
@@ -613,10 +623,11 @@ class AdamWTensors:
                     raise ValueError(f"{name} {i}: wrong size or device")
                 if size and name not in ("m_exp", "v_exp") and t.data_ptr() % 16:
                     raise ValueError(f"{name} {i} must be aligned to 16 bytes")
-                spans.append((t.data_ptr(), t.data_ptr() + size * t.element_size()))
+                if size:
+                    spans.append((t.data_ptr(), t.data_ptr() + size * t.element_size()))
             self._array[i] = _AdamWTensor(*(_p(t) for t in (p, w, g, a, b, ea, eb)), n)
         spans.sort()
-        if any(y[0] < x[1] for x, y in zip(spans, spans[1:]) if x[0] != x[1] and y[0] != y[1]):
+        if any(y[0] < x[1] for x, y in zip(spans, spans[1:])):
             raise ValueError("tensors overlap")
 
 
@@ -629,8 +640,10 @@ def grouter_adamw(tensors, hyper, grad_scale=None, stream=None):
         raise ValueError("hyper must hold 48 bytes")
     if grad_scale is not None and _dev(grad_scale, "grad_scale", torch.float32).numel() != 1:
         raise ValueError("grad_scale must have one element")
+    if not tensors.count:
+        return
     _check(lib().grouter_adamw(tensors._array, tensors.count, tensors.kind, tensors.grad_dtype, tensors.bits,
-                               ctypes.byref(hyper) if host else None, None if host else _p(hyper), _p(grad_scale), _stream(stream)),
+                               ctypes.byref(hyper) if host else None, None if host else _p(hyper), _p(grad_scale), _stream_for(tensors._held[0][0], stream)),
            "grouter_adamw")
 
 

@@ -513,13 +513,18 @@ bool ids_ok(const void* ids, int idx_dtype, int E) {
     if (idx_dtype == GROUTER_IDX_INT32) return ids && aligned_to(ids, 4);
     return ids && idx_dtype == GROUTER_IDX_UINT8 && E <= 256;
 }
-// a matrix of T rows of E elements, ld apart, whose byte offsets fit 63 bits
+// a matrix of T rows of E elements, ld apart, of at most 2^48 elements in all
 bool matrix_ok(const void* p, int dtype, int64_t ld, int64_t T, int E) {
     return p && type_ok(dtype) && aligned_to(p, type_bytes(dtype)) && T > 0 && T <= 0x7fffffff && E > 0 && E <= kMaxExperts && ld >= E &&
-           ld <= (1ll << 31);
+           ld <= (1ll << 31) && ld <= (1ll << 48) / T;
 }
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-    return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+// Whether two such matrices have no byte in common: they lie apart, or are different columns of rows of the same length.
+bool disjoint(const void* a, size_t row_a, size_t pitch_a, const void* b, size_t row_b, size_t pitch_b, int64_t T) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    if (x + (T - 1) * pitch_a + row_a <= y || y + (T - 1) * pitch_b + row_b <= x) return true;
+    if (pitch_a != pitch_b) return false;
+    const size_t behind = y >= x ? (y - x) % pitch_a : (pitch_a - (x - y) % pitch_a) % pitch_a;    // b's columns begin so far behind a's
+    return behind >= row_a && behind + row_b <= pitch_a;
 }
 }  // namespace
 
@@ -543,8 +548,8 @@ int grouter_route_bwd(const void* scores, int score_dtype, int64_t score_ld, int
     if (dlog_gate && (!dims_ok(T, k, E) || !ids_ok(topk_idx, idx_dtype, E) || !aligned_to(dlog_gate, 4))) return GROUTER_ERR_INVALID_ARG;
     if (coef && (S < 1 || S > kMaxSequences || (!seq_offsets && S != 1) || !aligned_to(coef, 4) || !aligned_to(seq_offsets, 8)))
         return GROUTER_ERR_INVALID_ARG;
-    const size_t span = ((size_t)(T - 1) * score_ld + E) * type_bytes(score_dtype), out_span = ((size_t)(T - 1) * dscore_ld + E) * type_bytes(dscore_dtype);
-    if (overlap(scores, span, dscores, out_span)) return GROUTER_ERR_INVALID_ARG;
+    const size_t size = type_bytes(score_dtype), out_size = type_bytes(dscore_dtype);
+    if (!disjoint(scores, E * size, score_ld * size, dscores, E * out_size, dscore_ld * out_size, T)) return GROUTER_ERR_INVALID_ARG;
     hipStream_t s = (hipStream_t)stream;
     PhaseTimer tm(GROUTER_PH_ROUTE_BWD, s);
     const hipError_t e = launch_route_bwd(scores, score_dtype, score_ld, T, E, gating, token_mask, topk_idx, idx_dtype, k, dlog_gate,

@@ -486,9 +486,10 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
             top = gate_shift(gating, group_max<L>(top));
             for (int j = part; j < k; j += L)
                 if (e[j] >= 0) z += gate_weight(gating, Type::widen(row[e[j]]), top);
-            const float each = sum * reciprocal_or_zero(group_sum<L>(z));
+            z = group_sum<L>(z);
+            // a quotient, not a product with 1 / z: the only one selected has a gate of exactly 1 and a gradient of exactly 0
             for (int j = part; j < k; j += L)
-                if (e[j] >= 0) u[j] -= each * gate_weight(gating, Type::widen(row[e[j]]), top);
+                if (e[j] >= 0 && z != 0.f) u[j] -= sum * (gate_weight(gating, Type::widen(row[e[j]]), top) / z);
         }
         if (sigmoid)
             for (int j = part; j < k; j += L)

@@ -283,6 +283,19 @@ def test_gradient_of_closed_experts_is_zero(gating):
     assert not torch.isnan(ds).any()
 
 
+def test_gradient_into_columns_of_the_same_matrix():
+    wide = torch.randn((300, 150), device=DEV)
+    s, ds = wide[:, 10:70], wide[:, 70:130]
+    keep = wide.clone()
+    out, _ = balance(s, s.topk(3, dim=1).indices.int(), b.GATE_SIGMOID, 1.0)
+    b.grouter_route_bwd(s, b.GATE_SIGMOID, ds, coef=out["coef"])
+    alone = torch.empty((300, 60), device=DEV)
+    b.grouter_route_bwd(keep[:, 10:70], b.GATE_SIGMOID, alone, coef=out["coef"])
+    assert torch.equal(ds, alone) and torch.equal(wide[:, :70], keep[:, :70]) and torch.equal(wide[:, 130:], keep[:, 130:])
+    with pytest.raises(b.GrouterError):
+        b.grouter_route_bwd(s, b.GATE_SIGMOID, wide[:, 69:129], coef=out["coef"])
+
+
 @pytest.mark.parametrize("gating", GATINGS)
 def test_gradient_is_the_differences_of_the_gates(gating):
     """L = sum a g over the gates in 64 bits, by differences of the oracle's gates; the kernel gets a g as the gradient by their logs."""
@@ -300,6 +313,17 @@ def test_gradient_is_the_differences_of_the_gates(gating):
             down[t, e] -= h
             diff = ((o.gates(up, ids, gating) - o.gates(down, ids, gating)) * a)[t].sum() / (2 * h)
             assert abs(diff - got[t, e]) <= 2 * FP * np.abs(q[t]).sum() + 1e-8
+
+
+@pytest.mark.parametrize("gating", [b.GATE_SOFTMAX_SELECTED, b.GATE_SIGMOID_NORMALISED])
+@pytest.mark.parametrize("E", [8, 60, 256])
+def test_gradient_of_the_only_selected_expert_is_zero(gating, E):
+    """Its gate is 1 whatever its score."""
+    s, ref = make_scores(500, E, torch.float32, E)
+    ids = torch.from_numpy(o.top_k(ref, 1).astype(np.int32)).to(DEV)
+    ds = torch.ones((500, E), device=DEV)
+    b.grouter_route_bwd(s, gating, ds, topk_idx=ids, dlog_gate=torch.randn((500, 1), device=DEV))
+    assert (ds == 0).all()
 
 
 # ---- gradient by the gates ----------------------------------------------------------------------------------------

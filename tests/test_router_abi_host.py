@@ -132,3 +132,32 @@ def test_binding_refuses_cpu_tensors_and_shapes():
 
 def test_phases_of_the_new_operators(L):
     assert b.PHASES[16:] == ("route", "route_bwd", "balance", "gate_bwd", "adamw")
+
+
+@pytest.mark.parametrize("ds,dld,ok", [(FAKE + 64 * 4, 128, True), (FAKE + 64 * 4 - 4, 128, False), (FAKE + 64 * 4 + 4, 128, False), (FAKE + 10 * 512 + 256, 128, True),
+                                       (FAKE - 256, 128, True), (FAKE - 252, 128, False), (FAKE + 64 * 4, 129, False), (FAKE + 3 * 512 + 256, 129, True)])
+def test_columns_of_one_matrix_do_not_overlap(L, ds, dld, ok):
+    """scores: four rows of 64 fp32 in rows of 128; refused calls return before the next check fails (S = 0), which both do."""
+    case = {**BWD, "ld": 128, "ds": ds, "dld": dld}
+    assert L.grouter_route_bwd(*{**case, "S": 0}.values()) == b.ERR_INVALID_ARG
+    if not ok:
+        assert L.grouter_route_bwd(*case.values()) == b.ERR_INVALID_ARG
+
+
+def test_tensors_and_stream_have_to_be_on_one_device(monkeypatch):
+    import torch
+
+    class On:
+        def __init__(self, index):
+            self.index = self.cuda_stream = index
+            self.device = self
+
+        def get_device(self):
+            return self.index
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(b, "_raw_stream", lambda: 77)
+    assert b._stream_for(On(0)) == 77 and b._stream_for(On(1), On(1)) == 1
+    for t, stream in ((On(1), None), (On(0), On(1))):
+        with pytest.raises(ValueError):
+            b._stream_for(t, stream)
