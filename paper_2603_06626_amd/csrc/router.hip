@@ -353,8 +353,8 @@ __device__ __forceinline__ int64_t offsets_up_to(const int64_t* __restrict__ off
     return lo;
 }
 
-// What the probabilities over all experts of a row are shares of, softmax or sigmoids, from what a lane holds; zero where it holds
-// nothing.  Returns what they are to be multiplied with.  The shift goes into the product with log2 e as a fused sum: its rounding is
+// What the probabilities over all experts of a row are shares of, softmax or sigmoids, for all that a lane fetched (an absent element has
+// the value that it has where it is present, and is left out of the sum).  Returns what they are to be multiplied with.  The shift goes into the product with log2 e as a fused sum: its rounding is
 // the same for all of a row, so no share depends on it.
 template <bool SIGMOID, class Type, int L, int V, bool FULL>
 __device__ __forceinline__ float shares(const Row<Type, L, V, FULL>& x, float (&share)[V]) {
@@ -363,7 +363,7 @@ __device__ __forceinline__ float shares(const Row<Type, L, V, FULL>& x, float (&
     for (int p = 0; p < x.N; ++p)
 #pragma unroll
         for (int w = 0; w < x.W; ++w) {
-            share[p * x.W + w] = x.has(p, w) ? x.at(p, w) : -INFINITY;
+            share[p * x.W + w] = !x.kShort || w < x.end ? x.at(p, w) : -INFINITY;     // (nothing was fetched behind a short row)
             top = fmaxf(top, share[p * x.W + w]);
         }
     top = group_max<L>(top);
@@ -377,7 +377,7 @@ __device__ __forceinline__ float shares(const Row<Type, L, V, FULL>& x, float (&
         for (int v = 0; v < V; ++v) share[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(share[v], 1.44269504f, -top));
     }
 #pragma unroll
-    for (int v = 0; v < V; ++v) z += share[v];
+    for (int v = 0; v < V; ++v) z += x.has(v / x.W, v % x.W) ? share[v] : 0.f;
     return reciprocal_or_zero(group_sum<L>(z));
 }
 
@@ -395,17 +395,17 @@ struct RouteGrad {
 };
 
 template <class Out, int W>
-__device__ __forceinline__ void store_piece(void* out, int64_t at, int skip, int end, const float* v) {
+__device__ __forceinline__ void store_piece(void* out, int64_t at, int end, const float* v) {
     auto* o = (typename Out::stored*)out + at;
     typename Out::stored q[W];
 #pragma unroll
     for (int w = 0; w < W; ++w) q[w] = Out::narrow(v[w]);
-    if (skip == 0 && end == W) {
+    if (end == W) {
         __builtin_memcpy(o, q, sizeof(q));
     } else {
 #pragma unroll
         for (int w = 0; w < W; ++w)
-            if (w >= skip && w < end) o[w] = q[w];
+            if (w < end) o[w] = q[w];
     }
 }
 
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
             x.fetch(p, coef, E, c + p * W);
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) dot += c[v] * prob[v];
+        for (int v = 0; v < V; ++v) dot += x.has(v / W, v % W) ? c[v] * prob[v] : 0.f;
         dot = group_sum<L>(dot) * scale;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -514,11 +514,11 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
 #pragma unroll
     for (int p = 0; p < N; ++p) {
         const int64_t at = t * a.out_ld + x.from[p];
-        const int skip = FULL ? 0 : x.skip[p], end = FULL ? W : x.end;
-        if (skip >= end) continue;
-        if (a.out_dtype == 0) store_piece<Fp32, W>(a.out, at, skip, end, ds + p * W);
-        else if (a.out_dtype == 1) store_piece<Bf16, W>(a.out, at, skip, end, ds + p * W);
-        else store_piece<Fp16, W>(a.out, at, skip, end, ds + p * W);
+        if (!FULL && x.skip[p] >= W) continue;     // no element of its own; others are written by both lanes that have them, alike
+        const int end = x.kShort ? x.end : W;
+        if (a.out_dtype == 0) store_piece<Fp32, W>(a.out, at, end, ds + p * W);
+        else if (a.out_dtype == 1) store_piece<Bf16, W>(a.out, at, end, ds + p * W);
+        else store_piece<Fp16, W>(a.out, at, end, ds + p * W);
     }
 }
 
