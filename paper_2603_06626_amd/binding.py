@@ -160,14 +160,33 @@ def _stream(stream=None):
     return _raw_stream()
 
 
-def _stream_for(t, stream=None):
-    """The stream to enqueue on: the given one, or the current one of the current device, which has to be the one that t is on."""
+def _find_current():
+    """(the current device, the handle of a device's current stream), from torch itself where it has them: its public functions look
+    after initialisation on every call, which a tensor on the GPU stands for."""
     import torch
 
-    device = torch.cuda.current_device() if stream is None else stream.device.index
-    if t.get_device() != device:
-        raise ValueError(f"the tensors are on device {t.get_device()}, the stream is device {device}'s")
-    return _stream(stream)
+    device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    handle = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return device, handle
+
+
+_current = None
+
+
+def _stream_for(t, stream=None):
+    """The stream to enqueue on: the given one, or the current one of the current device, which has to be the one that t is on."""
+    global _current
+    at = t.get_device()
+    if stream is not None:
+        device, handle = stream.device.index, stream.cuda_stream
+    else:
+        if _current is None:
+            _current = _find_current()
+        device = _current[0]()
+        handle = _current[1](device)
+    if at != device:
+        raise ValueError(f"the tensors are on device {at}, the stream is device {device}'s")
+    return handle
 
 
 def _dev(t, name, dtype=None):

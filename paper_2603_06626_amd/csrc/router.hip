@@ -1,72 +1,11 @@
-// The router of an expert layer: scores -> expert ids and gate weights (Eq. 2, r = g(TopK(s, k))), the way back, and the balance loss
-// with per-expert counts.
-//
-// All of them read a row of E scores per token.  A token belongs to a group of L neighbouring lanes, each of which holds V scores as
-// pieces of 16 bytes, piece p of lane i being number p L + i of the row: every load instruction of a group covers whole lines, and
-// every reduction over a row is one inside registers and log2(L) cross-lane moves.  V is 16 beyond 8 experts: few cross-lane steps
-// (each costs as much as one over all registers), and 64 / L tokens of a wave share the instructions of what follows.
-#include "lanes.hpp"
+// The router of an expert layer: scores -> expert ids and gate weights (Eq. 2, r = g(TopK(s, k))), and the way back.
+#include "router.hpp"
 
 namespace grouter {
 
 namespace {
 
 constexpr int kThreads = 256;
-
-enum Gating { kSoftmaxSelected = 0, kSoftmaxAll = 1, kSigmoid = 2, kSigmoidNormalised = 3 };
-
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
-__device__ __forceinline__ float shift_of(float top) { return top == -INFINITY ? 0.f : top; }   // a row of -inf shifts by nothing: all its terms are 0
-// sigmoid(x) * e^-shift, without overflow or loss on either side of 0
-__device__ __forceinline__ float sigmoid_of(float x, float shift = 0.f) {
-    return exp_of(fminf(x, 0.f) - shift) * __builtin_amdgcn_rcpf(1.f + exp_of(-fabsf(x)));
-}
-__device__ __forceinline__ float reciprocal_or_zero(float z) { return z == 0.f ? 0.f : 1.f / z; }
-
-template <class Type>
-constexpr int kPiece = 16 / sizeof(typename Type::stored);
-
-// What a lane holds of a row: N pieces of W columns.  A piece that would reach behind column E is fetched from earlier columns, so that
-// only the row's own elements are read, and its first `skip` elements count as absent (they belong to the piece before).  Rows
-// shorter than a piece are fetched one by one.  Addresses need no more than the elements' own alignment.  FULL: E = L V, nothing is
-// absent and nothing has to be compared for it.
-template <class Type, int L, int V, bool FULL>
-struct Row {
-    static constexpr int W = kPiece<Type>, N = V / W;
-    static constexpr bool kShort = L == 1 && V == 8 && !FULL;     // E may be less than a piece
-    typename Type::stored raw[N][W];
-    int from[N], skip[N], end;     // columns from .. from + W - 1, elements skip .. end - 1 present
-    __device__ __forceinline__ void place(int part, int E) {
-        end = kShort ? min(E, W) : W;
-#pragma unroll
-        for (int p = 0; p < N; ++p) {
-            const int start = (p * L + part) * W;
-            from[p] = FULL ? start : max(0, min(start, E - W));
-            skip[p] = FULL ? 0 : min(start - from[p], W);
-        }
-    }
-    // W elements of a row of anything, where the lane's piece p is
-    template <class T>
-    __device__ __forceinline__ void fetch(int p, const T* __restrict__ row, int E, T* out) const {
-        if (kShort && E < W) {
-#pragma unroll
-            for (int w = 0; w < W; ++w) out[w] = w < E ? row[w] : T(0);
-        } else {
-            __builtin_memcpy(out, row + from[p], W * sizeof(T));
-        }
-    }
-    __device__ __forceinline__ void load(const typename Type::stored* __restrict__ row, int E) {
-#pragma unroll
-        for (int p = 0; p < N; ++p) fetch(p, row, E, raw[p]);
-    }
-    __device__ __forceinline__ bool has(int p, int w) const { return FULL || (w >= skip[p] && (!kShort || w < end)); }
-    // where column e stands when all lanes' pieces are put side by side: in the last piece that is not whole, behind the absent ones
-    static __device__ __forceinline__ int place_of(int e, int E) {
-        const int whole = E / W * W;
-        return FULL || E < W || e < whole ? e : e + W - E % W;
-    }
-    __device__ __forceinline__ float at(int p, int w) const { return Type::widen(raw[p][w]); }
-};
 
 // ---- keys: whole numbers, all different within a row, that order like the scores and among equal scores by the lower column -------
 // A score's bits become a two's complement number (-0 and +0 both 0), moved up by the distance of the largest positive NaN from the
@@ -323,64 +262,6 @@ __global__ __launch_bounds__(kThreads) void k_route_rounds(const typename Type::
     for (int j = part; j < k; j += L) out.put(t * k + j, pick[j], masked ? 0.f : gate_weight(gating, Type::widen(row[pick[j]]), top) * scale);
 }
 
-__device__ __forceinline__ int id_of(const void* ids, int idx_dtype, int64_t i) {
-    return idx_dtype == 1 ? (int)((const uint8_t*)ids)[i] : (int)((const int32_t*)ids)[i];
-}
-
-// v of one lane, the same for all: a scalar
-__device__ __forceinline__ int64_t of_lane(int64_t v, int lane) {
-    const uint32_t low = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane), high = (uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane);
-    return (int64_t)((uint64_t)high << 32 | low);
-}
-
-// How many of the S + 1 ascending offsets are at most t, t the same in all lanes, and the offset after them (INT64_MAX behind the last):
-// 64 probes at a time, so up to 63 sequences take a single load.  Sequence s holds the tokens [off[s], off[s + 1]).
-__device__ __forceinline__ int64_t offsets_up_to(const int64_t* __restrict__ off, int64_t S, int64_t t, int64_t& next) {
-    const int lane = threadIdx.x & 63;
-    int64_t lo = 0, hi = S + 1;
-    next = INT64_MAX;
-    while (lo < hi) {
-        const int64_t step = (hi - lo + 63) / 64, probe = lo + (lane + 1) * step - 1;
-        const int64_t value = probe < hi ? off[probe] : INT64_MAX;
-        const int passed = __popcll(__ballot(value <= t));
-        if (passed < 64) {
-            const int64_t above = of_lane(value, passed);
-            if (above != INT64_MAX) next = above;     // else the one that an earlier round of probes found
-        }
-        lo += passed * step;
-        hi = min(hi, lo + step - 1);
-    }
-    return lo;
-}
-
-// What the probabilities over all experts of a row are shares of, softmax or sigmoids, for all that a lane fetched (an absent element has
-// the value that it has where it is present, and is left out of the sum).  Returns what they are to be multiplied with.  The shift goes into the product with log2 e as a fused sum: its rounding is
-// the same for all of a row, so no share depends on it.
-template <bool SIGMOID, class Type, int L, int V, bool FULL>
-__device__ __forceinline__ float shares(const Row<Type, L, V, FULL>& x, float (&share)[V]) {
-    float top = -INFINITY, z = 0.f;
-#pragma unroll
-    for (int p = 0; p < x.N; ++p)
-#pragma unroll
-        for (int w = 0; w < x.W; ++w) {
-            share[p * x.W + w] = !x.kShort || w < x.end ? x.at(p, w) : -INFINITY;     // (nothing was fetched behind a short row)
-            top = fmaxf(top, share[p * x.W + w]);
-        }
-    top = group_max<L>(top);
-    if (SIGMOID) {
-        top = shift_of(fminf(top, 0.f));
-#pragma unroll
-        for (int v = 0; v < V; ++v) share[v] = sigmoid_of(share[v], top);
-    } else {
-        top = shift_of(top) * 1.44269504f;
-#pragma unroll
-        for (int v = 0; v < V; ++v) share[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(share[v], 1.44269504f, -top));
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) z += x.has(v / x.W, v % x.W) ? share[v] : 0.f;
-    return reciprocal_or_zero(group_sum<L>(z));
-}
-
 struct RouteGrad {
     const void* ids;             // k ids per token with the gradients by the logs of their gates, or null
     int idx_dtype, k;
@@ -522,348 +403,6 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
     }
 }
 
-// ---- balance loss -------------------------------------------------------------------------------------------------------------
-// Per sequence s of n tokens: f_e = count_e / (k n), P_e = mean of p_e, loss = alpha E sum_e f_e P_e, and what the gradient needs,
-// coef_e = alpha E f_e / n.  The tokens are cut into chunks of equal length, one per workgroup; the part of a sequence inside a chunk
-// leaves its sums in a slot of its own, chunk + sequence (both only grow along the tokens, so no two parts share one), and a second
-// launch adds up each sequence's slots in order.  So work is even whatever the sequences' lengths, and no float is added atomically.
-struct BalanceCell {
-    float prob;
-    int32_t count;
-};
-struct BalanceParts {
-    BalanceCell* cells;  // [chunks + S][E]
-    int32_t* tokens;     // [chunks + S], valid ones
-    double* loss;        // [S][column blocks]
-    uint32_t* done;      // workgroups that have left their loss
-    int64_t rows;        // of a chunk
-};
-
-constexpr int kPartThreads = 256;
-constexpr int kAloneRounds = 4;
-
-struct BalanceOut {
-    float alpha;
-    int32_t* counts;
-    float *prob, *coef, *loss;
-    // results of one expert in a sequence with these sums; its part of the loss
-    __device__ __forceinline__ double put(int64_t at, int E, int k, int tokens, double sum, int count) const {
-        const double over = 1.0 / max(tokens, 1), mean = sum * over, scaled = (double)alpha * E / k * over * count;
-        counts[at] = count;
-        prob[at] = (float)mean;
-        coef[at] = (float)(scaled * over);
-        return scaled * mean;
-    }
-};
-
-template <int STEP>
-__device__ __forceinline__ float rotated(float v) { return __uint_as_float(dpp_move<0x120 + STEP>(__float_as_uint(v))); }   // row_ror
-
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-    for (int step = 32; step > 0; step /= 2) v += __shfl_xor(v, step);
-    return v;
-}
-
-// A chunk is walked in tiles of as many tokens as the workgroup has groups of lanes.  While a tile lies within one sequence, its rows are
-// added up in registers; where a sequence ends, the sums of the lanes are joined through LDS (flush).  Sequences that begin and end
-// inside one tile are added up from a copy of the tile's rows in LDS, each by a wave of its own.
-// ALONE: one workgroup takes all tokens of the only sequence and writes the results itself.
-template <class Type, int L, int V, bool FULL, bool SIGMOID, bool ALONE>
-__global__ __launch_bounds__(kPartThreads) void k_balance_parts(const typename Type::stored* __restrict__ scores, int64_t ld, int64_t T, int E, int k,
-                                                                const uint8_t* __restrict__ token_mask,
-                                                                const void* __restrict__ ids, int idx_dtype,
-                                                                const int64_t* __restrict__ off, int64_t S, BalanceParts parts, BalanceOut out) {
-    constexpr int kWaves = kPartThreads / 64, kTokens = kPartThreads / L, C = L * V, W = kPiece<Type>;
-    constexpr int kAhead = L >= 8 ? 1 : L >= 4 ? 2 : 4;      // ids of a tile that a thread fetches ahead: 8 per token, shared by its lanes
-    constexpr int kRows = L <= 16 ? 4 : 64 / L;      // partial sums that a wave leaves in LDS: one per 16 lanes, or per group
-    constexpr int kSpan = 64 / kRows;
-    __shared__ float s_rows[kTokens * C];            // a tile's rows, or the waves' partial sums, as the pieces that the lanes hold
-    __shared__ int s_count[C], s_tokens[2];
-    __shared__ int16_t s_ids[kAhead * kPartThreads];  // with a tile's rows, the ids of its first slots
-    __shared__ uint32_t s_few[kWaves][C / 2];        // counts of a sequence inside one tile (at most 4096 slots), two in a word
-    static_assert(kWaves * kRows <= kTokens, "partial sums fit where the rows do");
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane % L;
-    const int64_t row0 = blockIdx.x * parts.rows, row1 = min(T, row0 + parts.rows);
-    if (!ALONE && blockIdx.x == 0 && threadIdx.x == 0) *parts.done = 0;
-    for (int e = threadIdx.x; e < C; e += kPartThreads) s_count[e] = 0;
-    if (threadIdx.x < 2) s_tokens[threadIdx.x] = 0;
-    Row<Type, L, V, FULL> x, ahead;
-    x.place(part, E);
-    ahead = x;
-    ahead.load(scores + min(row0 + threadIdx.x / L, row1 - 1) * ld, E);
-    // the walk is in sequence s, whose tokens end before `next`; -1 and S: in none
-    int64_t s = 0, next = T;
-    if (off) s = offsets_up_to(off, S, row0, next) - 1;
-    int64_t window = s + 1, ends = off ? off[min(window + 1 + lane, S)] : 0;     // lane i: the end of sequence window + i
-    double loss = 0.0;
-    bool empty = true, open = false;     // no sequence has been joined yet; the present one has tokens that are not joined
-    float sum[V];
-    int tokens = 0, turn = 0;
-#pragma unroll
-    for (int v = 0; v < V; ++v) sum[v] = 0.f;
-    auto emit = [&](int64_t seq, int e, int n, float total, int count) {
-        if (ALONE) loss += out.put(seq * E + e, E, k, n, total, count);
-        else parts.cells[(blockIdx.x + seq) * E + e] = BalanceCell{total, count};
-    };
-    __syncthreads();
-    for (int64_t t0 = row0; t0 < row1; t0 += kTokens) {
-        const int64_t t = t0 + threadIdx.x / L, t1 = min(t0 + kTokens, row1);
-        const bool live = t < row1 && !(token_mask && token_mask[t] == 0);
-        x = ahead;
-        if (t1 < row1) ahead.load(scores + min(t + kTokens, row1 - 1) * ld, E);
-        // the tile's first ids while its probabilities are computed
-        const uint32_t slots = (uint32_t)(t1 - t0) * (uint32_t)k;
-        auto counted = [&](uint32_t i) {
-            const int id = i < slots && !(token_mask && token_mask[t0 + i / (uint32_t)k] == 0) ? id_of(ids, idx_dtype, t0 * k + i) : -1;
-            return (unsigned)id < (unsigned)E ? id : -1;
-        };
-        int id[kAhead];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) id[i] = counted(threadIdx.x + i * kPartThreads);
-        float p[V];
-        if (!FULL) {     // compared in every tile: masks that wait for the next one would fill the scalar registers
-#pragma unroll
-            for (int i = 0; i < x.N; ++i) asm volatile("" : "+v"(x.skip[i]));
-        }
-        float scale = shares<SIGMOID>(x, p);
-        if (__ballot(!live)) {     // (what a padding token holds may be NaN)
-            scale = live ? scale : 0.f;
-#pragma unroll
-            for (int v = 0; v < V; ++v) p[v] = live ? p[v] : 0.f;
-        }
-        int64_t u = t0;      // the tile's tokens before u are done
-        for (;;) {
-            const int64_t w = min(next, t1);
-            if (s >= 0 && s < S && u < w) {
-                open = true;
-                const bool in = live && t >= u && t < w;
-                const float take = in ? scale : 0.f;
-                if ((u == t0 && w == t1) || __ballot(in) == ~0ull) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v) sum[v] = __builtin_fmaf(p[v], take, sum[v]);
-                } else {     // another sequence's NaN stays its own
-#pragma unroll
-                    for (int v = 0; v < V; ++v) sum[v] += in ? p[v] * scale : 0.f;
-                }
-                tokens += in;
-                const uint32_t lo = (uint32_t)(u - t0) * (uint32_t)k, hi = (uint32_t)(w - t0) * (uint32_t)k;
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) {
-                    const uint32_t at = threadIdx.x + i * kPartThreads;
-                    if (id[i] >= 0 && at >= lo && at < hi) atomicAdd(&s_count[id[i]], 1);
-                }
-                for (uint32_t i = threadIdx.x + kAhead * kPartThreads; i < hi; i += kPartThreads) {
-                    const int e = i >= lo ? counted(i) : -1;
-                    if (e >= 0) atomicAdd(&s_count[e], 1);
-                }
-            }
-            if (open && (next < t1 || t1 == row1)) {     // the sequence or the chunk ends
-                open = empty = false;
-                if (part == 0 && tokens) atomicAdd(&s_tokens[turn], tokens);
-                // over the groups within 16 lanes in registers, over the rest in LDS
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    if constexpr (L <= 1) sum[v] += rotated<1>(sum[v]);
-                    if constexpr (L <= 2) sum[v] += rotated<2>(sum[v]);
-                    if constexpr (L <= 4) sum[v] += rotated<4>(sum[v]);
-                    if constexpr (L <= 8) sum[v] += rotated<8>(sum[v]);
-                    if (lane % kSpan < L) s_rows[(wave * kRows + lane / kSpan) * C + (v / W * L + part) * W + v % W] = sum[v];
-                    sum[v] = 0.f;
-                }
-                tokens = 0;
-                __syncthreads();
-                const int n = s_tokens[turn];
-                for (int e = threadIdx.x; e < E; e += kPartThreads) {
-                    float all = 0.f;
-                    const float* rows = s_rows + x.place_of(e, E);
-#pragma unroll 8
-                    for (int w = 0; w < kWaves * kRows; ++w) all += rows[w * C];
-                    emit(s, e, n, all, s_count[e]);
-                    s_count[e] = 0;
-                }
-                if (!ALONE && threadIdx.x == 0) parts.tokens[blockIdx.x + s] = n;
-                turn ^= 1;
-                if (threadIdx.x == 0) s_tokens[turn] = 0;
-                __syncthreads();
-            }
-            if (next >= t1) break;
-            u = max(next, t0);
-            bool copied = false;
-            int whose = 0;
-            for (++s; s < S; ++s) {
-                if (s - window >= 64) {
-                    window = s;
-                    ends = off[min(window + 1 + lane, S)];
-                }
-                next = of_lane(ends, (int)(s - window));
-                if (next >= t1) break;
-                if (next > u) {
-                    empty = false;
-                    if (!copied) {
-                        copied = true;
-#pragma unroll
-                        for (int v = 0; v < V; ++v)
-                            s_rows[threadIdx.x / L * C + (v / W * L + part) * W + v % W] = p[v] * scale;
-#pragma unroll
-                        for (int i = 0; i < kAhead; ++i) s_ids[threadIdx.x + i * kPartThreads] = (int16_t)id[i];
-                        __syncthreads();
-                    }
-                    if (whose == wave) {
-                        uint32_t* few = s_few[wave];
-                        for (int e = lane; e < C / 2; e += 64) few[e] = 0;
-                        int n = 0;
-                        const int a = (int)(u - t0), b = (int)(next - t0);
-                        for (int i = a; i < b; i += 64) n += __popcll(__ballot(i + lane < b && !(token_mask && token_mask[t0 + min(i + lane, b - 1)] == 0)));
-                        for (uint32_t i = (uint32_t)a * k + lane; i < (uint32_t)b * k; i += 64) {
-                            const int e = i < kAhead * kPartThreads ? s_ids[i] : counted(i);
-                            if (e >= 0) atomicAdd(&few[e >> 1], 1u << (16 * (e & 1)));
-                        }
-                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                        for (int e = lane; e < E; e += 64) {
-                            float all = 0.f;
-                            const float* rows = s_rows + x.place_of(e, E);
-#pragma unroll 8
-                            for (int i = a; i < b; ++i) all += rows[i * C];
-                            emit(s, e, n, all, (int)(few[e >> 1] >> (16 * (e & 1)) & 0xffffu));
-                        }
-                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                        if (!ALONE && lane == 0) parts.tokens[blockIdx.x + s] = n;
-                    }
-                    whose = whose + 1 == kWaves ? 0 : whose + 1;
-                    u = next;
-                }
-            }
-            if (s >= S) next = INT64_MAX;
-            if (copied) __syncthreads();
-        }
-    }
-    if (ALONE) {
-        __shared__ double s_loss[kWaves];
-        if (empty)
-            for (int e = threadIdx.x; e < E; e += kPartThreads) out.put(e, E, k, 0, 0.0, 0);
-        loss = wave_sum(loss);
-        if (lane == 0) s_loss[wave] = loss;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int w = 1; w < kWaves; ++w) loss += s_loss[w];
-            *out.loss = (float)loss;
-        }
-    }
-}
-
-// Joins the slots of one sequence for COLUMNS experts; THREADS / COLUMNS threads share the slots of an expert.
-template <int COLUMNS, int THREADS>
-__global__ __launch_bounds__(THREADS) void k_balance_join(int64_t T, int E, int k, const uint8_t* __restrict__ token_mask,
-                                                          const int64_t* __restrict__ off, int64_t S, BalanceParts parts, BalanceOut out) {
-    constexpr int kWaves = THREADS / 64, kDeals = THREADS / COLUMNS;
-    __shared__ double s_sum[kWaves][COLUMNS];
-    __shared__ int s_count[kWaves][COLUMNS], s_tokens[kWaves];
-    __shared__ bool s_last;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t s = blockIdx.x;
-    const int64_t begin = off ? max((int64_t)0, off[s]) : 0, end = off ? min(T, off[s + 1]) : T;
-    const int64_t c0 = begin / parts.rows, c1 = begin < end ? (end - 1) / parts.rows + 1 : c0;
-    const int col = threadIdx.x % COLUMNS, e = blockIdx.y * COLUMNS + col;
-    double sum = 0.0;
-    int count = 0, tokens = 0;
-    if (e < E)
-#pragma unroll 8
-        for (int64_t c = c0 + threadIdx.x / COLUMNS; c < c1; c += kDeals) {
-            const BalanceCell cell = parts.cells[(c + s) * E + e];
-            sum += (double)cell.prob;
-            count += cell.count;
-        }
-    if (token_mask)
-        for (int64_t c = c0 + threadIdx.x; c < c1; c += THREADS) tokens += parts.tokens[c + s];
-#pragma unroll
-    for (int step = COLUMNS; step < 64; step *= 2) {
-        sum += __shfl_xor(sum, step);
-        count += __shfl_xor(count, step);
-    }
-    if (token_mask)
-#pragma unroll
-        for (int step = 1; step < 64; step *= 2) tokens += __shfl_xor(tokens, step);
-    if (lane < COLUMNS) {
-        s_sum[wave][lane] = sum;
-        s_count[wave][lane] = count;
-    }
-    if (lane == 0) s_tokens[wave] = tokens;
-    __syncthreads();
-    if (wave == 0) {
-        double part = 0.0;
-        if (lane < COLUMNS) {
-            for (int w = 1; w < kWaves; ++w) {
-                sum += s_sum[w][lane];
-                count += s_count[w][lane];
-            }
-        }
-        if (token_mask) {
-            tokens = 0;
-            for (int w = 0; w < kWaves; ++w) tokens += s_tokens[w];
-        } else {
-            tokens = (int)max((int64_t)0, end - begin);
-        }
-        if (lane < COLUMNS && e < E) part = out.put(s * E + e, E, k, tokens, sum, count);
-        part = wave_sum(part);
-        if (gridDim.x == 1 && gridDim.y == 1) {
-            if (lane == 0) *out.loss = (float)part;
-        } else if (lane == 0) {
-            __hip_atomic_store(parts.loss + s * gridDim.y + blockIdx.y, part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            s_last = __hip_atomic_fetch_add(parts.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1 == gridDim.x * gridDim.y;
-        }
-    }
-    if (gridDim.x == 1 && gridDim.y == 1) return;
-    __syncthreads();
-    if (!s_last) return;
-    // the workgroup that finishes last adds up all losses, in their order whichever it is
-    double all = 0.0;
-    for (int64_t i = threadIdx.x; i < S * gridDim.y; i += THREADS) all += __hip_atomic_load(parts.loss + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    all = wave_sum(all);
-    __syncthreads();
-    if (lane == 0) s_sum[wave][0] = all;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kWaves; ++w) all += s_sum[w][0];
-        *out.loss = (float)all;
-    }
-}
-
-template <bool B>
-struct Flag {
-    static constexpr bool value = B;
-};
-// Calls f with the lanes per token and the scores per lane that E experts take, and whether E fills them.
-template <class F>
-hipError_t with_lanes(int E, F f) {
-#define GROUTER_LANES(L, V)                                                                                         \
-    if (E == L * V) return f(std::integral_constant<int, L>{}, std::integral_constant<int, V>{}, Flag<true>{});     \
-    if (E < L * V) return f(std::integral_constant<int, L>{}, std::integral_constant<int, V>{}, Flag<false>{})
-    GROUTER_LANES(1, 8);
-    GROUTER_LANES(1, 16);
-    GROUTER_LANES(2, 16);
-    GROUTER_LANES(4, 16);
-    GROUTER_LANES(8, 16);
-    GROUTER_LANES(16, 16);
-    GROUTER_LANES(32, 16);
-    GROUTER_LANES(64, 16);
-#undef GROUTER_LANES
-    return hipErrorInvalidValue;
-}
-template <class F>
-hipError_t with_flag(bool b, F f) { return b ? f(Flag<true>{}) : f(Flag<false>{}); }
-int lanes_of(int E) {
-    int l = 1;
-    while (l * 16 < E) l *= 2;
-    return l;
-}
-template <class F>
-hipError_t with_type(int dtype, F f) {
-    if (dtype == 0) return f(Fp32{});
-    if (dtype == 1) return f(Bf16{});
-    return f(Fp16{});
-}
-
 }  // namespace
 
 hipError_t launch_route(const void* scores, int dtype, int64_t ld, int64_t T, int E, int k, int gating, const uint8_t* token_mask, void* ids,
@@ -906,60 +445,6 @@ hipError_t launch_route_bwd(const void* scores, int dtype, int64_t ld, int64_t T
             });
         });
     });
-}
-
-// Chunks: a few per CU at most, so that a sequence's slots are few, and not below the tokens that a workgroup takes at a time.
-BalanceLayout balance_layout(int64_t T, int E, int64_t S) {
-    BalanceLayout l{};
-    const int64_t at_once = kPartThreads / lanes_of(E), rows = (T + 511) / 512;
-    l.rows = (rows + at_once - 1) / at_once * at_once;
-    l.chunks = (T + l.rows - 1) / l.rows;
-    const size_t slots = (size_t)(l.chunks + S);
-    size_t o = 0;
-    auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
-    l.done = take(256);
-    l.loss = take(sizeof(double) * (size_t)S * ((size_t)(E + 15) / 16));
-    l.tokens = take(sizeof(int32_t) * slots);
-    l.cells = take(sizeof(BalanceCell) * slots * (size_t)E);
-    l.total = o;
-    return l;
-}
-
-hipError_t launch_balance(const void* scores, int dtype, int64_t ld, int64_t T, int E, int k, bool sigmoid, const uint8_t* token_mask, const void* ids,
-                          int idx_dtype, const int64_t* off, int64_t S, float alpha, int32_t* counts, float* prob, float* coef,
-                          float* loss, void* ws, hipStream_t s) {
-    const BalanceLayout l = balance_layout(T, E, S);
-    char* w = (char*)ws;
-    const BalanceParts parts{(BalanceCell*)(w + l.cells), (int32_t*)(w + l.tokens), (double*)(w + l.loss), (uint32_t*)(w + l.done), l.rows};
-    const BalanceOut out{alpha, counts, prob, coef, loss};
-    // one workgroup and no second launch where it needs few rounds: see kAloneRounds
-    const bool alone = S == 1 && T <= (int64_t)kAloneRounds * kPartThreads / lanes_of(E);
-    BalanceParts whole = parts;
-    if (alone) whole.rows = T;
-    const hipError_t e = with_type(dtype, [&](auto type) {
-        return with_lanes(E, [&](auto lanes, auto v, auto full) {
-            return with_flag(sigmoid, [&](auto flag) {
-                typedef decltype(type) Type;
-                constexpr int L = decltype(lanes)::value, V = decltype(v)::value;
-                constexpr bool FULL = decltype(full)::value, SIGMOID = decltype(flag)::value;
-                const auto* x = (const typename Type::stored*)scores;
-                if (alone)
-                    hipLaunchKernelGGL((k_balance_parts<Type, L, V, FULL, SIGMOID, true>), dim3(1), dim3(kPartThreads), 0, s, x, ld, T, E, k, token_mask,
-                                       ids, idx_dtype, off, S, whole, out);
-                else
-                    hipLaunchKernelGGL((k_balance_parts<Type, L, V, FULL, SIGMOID, false>), dim3((unsigned)l.chunks), dim3(kPartThreads), 0, s, x, ld, T, E,
-                                       k, token_mask, ids, idx_dtype, off, S, parts, out);
-                return hipGetLastError();
-            });
-        });
-    });
-    if (e != hipSuccess || alone) return e;
-    // many slots per sequence: 64 threads to an expert's; few: 4
-    if (S < 8)
-        hipLaunchKernelGGL((k_balance_join<16, 1024>), dim3((unsigned)S, (unsigned)(E + 15) / 16), dim3(1024), 0, s, T, E, k, token_mask, off, S, parts, out);
-    else
-        hipLaunchKernelGGL((k_balance_join<64, 256>), dim3((unsigned)S, (unsigned)(E + 63) / 64), dim3(256), 0, s, T, E, k, token_mask, off, S, parts, out);
-    return hipGetLastError();
 }
 
 }  // namespace grouter

@@ -145,8 +145,6 @@ def test_columns_of_one_matrix_do_not_overlap(L, ds, dld, ok):
 
 
 def test_tensors_and_stream_have_to_be_on_one_device(monkeypatch):
-    import torch
-
     class On:
         def __init__(self, index):
             self.index = self.cuda_stream = index
@@ -155,8 +153,7 @@ def test_tensors_and_stream_have_to_be_on_one_device(monkeypatch):
         def get_device(self):
             return self.index
 
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    monkeypatch.setattr(b, "_raw_stream", lambda: 77)
+    monkeypatch.setattr(b, "_current", (lambda: 0, lambda device: 77 + device))
     assert b._stream_for(On(0)) == 77 and b._stream_for(On(1), On(1)) == 1
     for t, stream in ((On(1), None), (On(0), On(1))):
         with pytest.raises(ValueError):
