@@ -94,21 +94,43 @@ __device__ __forceinline__ void sort_list(typename K::Key (&x)[8]) {
     exchange<K, 1, 4>(x); exchange<K, 3, 6>(x);
     exchange<K, 1, 2>(x); exchange<K, 3, 4>(x); exchange<K, 5, 6>(x);
 }
-// x becomes the largest of two lists, each sorted: the larger of x[i] and y[last - i] are they, and rise and fall once
-template <class K>
-__device__ __forceinline__ void merge_list(typename K::Key (&x)[4], const typename K::Key (&y)[4]) {
+// sorts N keys that rise and fall once
+template <class K, int N>
+__device__ __forceinline__ void sort_bitonic(typename K::Key* x) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = K::larger(x[i], y[3 - i]);
-    exchange<K, 0, 2>(x); exchange<K, 1, 3>(x);
-    exchange<K, 0, 1>(x); exchange<K, 2, 3>(x);
+    for (int step = N / 2; step > 0; step /= 2)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (!(i & step)) {
+                const auto a = x[i], b = x[i + step];
+                x[i] = K::larger(a, b);
+                x[i + step] = K::smaller(a, b);
+            }
 }
 template <class K>
-__device__ __forceinline__ void merge_list(typename K::Key (&x)[8], const typename K::Key (&y)[8]) {
+__device__ __forceinline__ void sort_list(typename K::Key (&x)[16]) {
+    typename K::Key a[8], b[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = K::larger(x[i], y[7 - i]);
-    exchange<K, 0, 4>(x); exchange<K, 1, 5>(x); exchange<K, 2, 6>(x); exchange<K, 3, 7>(x);
-    exchange<K, 0, 2>(x); exchange<K, 1, 3>(x); exchange<K, 4, 6>(x); exchange<K, 5, 7>(x);
-    exchange<K, 0, 1>(x); exchange<K, 2, 3>(x); exchange<K, 4, 5>(x); exchange<K, 6, 7>(x);
+    for (int i = 0; i < 8; ++i) {
+        a[i] = x[i];
+        b[i] = x[8 + i];
+    }
+    sort_list<K>(a);
+    sort_list<K>(b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        x[i] = K::larger(a[i], b[7 - i]);
+        x[8 + i] = K::smaller(a[i], b[7 - i]);
+    }
+    sort_bitonic<K, 8>(x);
+    sort_bitonic<K, 8>(x + 8);
+}
+// x becomes the largest of two lists, each sorted: the larger of x[i] and y[last - i] are they, and rise and fall once
+template <class K, int M>
+__device__ __forceinline__ void merge_list(typename K::Key (&x)[M], const typename K::Key (&y)[M]) {
+#pragma unroll
+    for (int i = 0; i < M; ++i) x[i] = K::larger(x[i], y[M - 1 - i]);
+    sort_bitonic<K, M>(x);
 }
 template <class K, int L, int M, int STEP = 1>
 __device__ __forceinline__ void merge_group(typename K::Key (&x)[M]) {
@@ -154,8 +176,9 @@ __device__ __forceinline__ float gate_shift(int gating, float largest) {
 }
 
 // Ids and gates, k <= M.  A lane sorts its keys in lists of M, merges them to their M largest, and log2(L) more merges with its partners'
-// lists leave every lane of the group with the row's.  No branch, no memory in between: for 128 experts, k = 8 and 16-bit scores about
-// 25 of the 60 instructions per token; k rounds of a maximum over the group take twice as many.
+// lists leave every lane of the group with the row's, without a branch or memory in between.  262144 tokens, E = 128, k = 8: 21.3 us with
+// bf16 scores (3.4 TB/s; the copy rate would allow 15: what is left is the comparisons), 35 with fp32 ones (4.2 TB/s); k rounds of a
+// maximum over the group took 51.6 us with bf16.
 template <class Type, int L, int V, bool FULL, int M>
 __global__ __launch_bounds__(kThreads) void k_route_lists(const typename Type::stored* __restrict__ scores, int64_t ld, int64_t T, int E, int k,
                                                           int gating, const uint8_t* __restrict__ token_mask, RouteOut out) {
@@ -417,7 +440,12 @@ hipError_t launch_route(const void* scores, int dtype, int64_t ld, int64_t T, in
             const auto* x = (const typename Type::stored*)scores;
             if (k <= 4) hipLaunchKernelGGL((k_route_lists<Type, L, V, FULL, 4>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
             else if (k <= 8) hipLaunchKernelGGL((k_route_lists<Type, L, V, FULL, 8>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
-            else hipLaunchKernelGGL((k_route_rounds<Type, L, V, FULL>), grid, threads, tokens * k * sizeof(uint16_t), s, x, ld, T, E, k, gating, token_mask, out);
+            else if (V == 16 && k <= 16 && (dtype == 0 || E <= 256 || k > 12)) {
+                // Lists of 16 cost the same for 9 and for 16 experts, rounds grow with k (262144 tokens; rounds / lists in us): E = 128, k = 10
+                // 38 / 35 with bf16 and 71 / 49 with fp32 scores, k = 16 52 / 35 and 98 / 49; bf16, E = 256 73 / 76 and 98 / 75; a quarter of
+                // the tokens with E = 512 37 / 43 and 52 / 43, with E = 1024 74 / 92 and 100 / 91; fp32, E = 1024 138 / 131 and 200 / 127.
+                if constexpr (V == 16) hipLaunchKernelGGL((k_route_lists<Type, L, V, FULL, 16>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
+            } else hipLaunchKernelGGL((k_route_rounds<Type, L, V, FULL>), grid, threads, tokens * k * sizeof(uint16_t), s, x, ld, T, E, k, gating, token_mask, out);
             return hipGetLastError();
         });
     });

@@ -52,7 +52,9 @@ def check_route(s, ref, k, gating, ids=torch.int32, mask=None):
 
 # every number of lanes per token, full and ragged, with vector and single loads
 SIZES = [(1, 1, 1), (3, 2, 2), (70, 7, 3), (67, 8, 8), (300, 8, 2), (33, 9, 4), (5, 16, 1), (40, 17, 5), (19, 33, 6), (67, 60, 5), (30, 64, 6), (18, 65, 7),
-         (35, 128, 8), (9, 129, 4), (9, 256, 8), (5, 257, 3), (5, 300, 70), (5, 512, 8), (3, 513, 9), (3, 1000, 8), (2, 1024, 5)]
+         (35, 128, 8), (9, 129, 4), (9, 256, 8), (5, 257, 3), (5, 300, 70), (5, 512, 8), (3, 513, 9), (3, 1000, 8), (2, 1024, 5),
+         # both sides of the lines between forms: lists of 4, 8 and 16, rounds
+         (33, 16, 16), (20, 64, 9), (20, 64, 16), (20, 64, 17), (9, 256, 12), (5, 300, 12), (5, 300, 13), (5, 512, 16), (3, 1024, 16), (3, 1024, 17)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
