@@ -1,7 +1,9 @@
 // One AdamW step over many tensors: with g the scaled gradient,
 //   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  w = w - (lr wd w + lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)).
 //
-// A pass over memory and nothing else: 22 to 30 bytes per element with 32-bit moments, 10 to 18 with 8-bit ones.  A launch takes the
+// A pass over memory and little else: 22 to 30 bytes per element with 32-bit moments, 10 to 18 with 8-bit ones.  554 M elements with fp32
+// masters and moments and bf16 gradients 2.88 ms (5.4 TB/s; a large copy reaches 4.8), in bf16 with 8-bit moments 1.02 to 1.07 ms (5.2 to
+// 5.5 TB/s, with the vector units nearly as busy as the memory).  A launch takes the
 // addresses of up to kAdamwPerLaunch tensors in its arguments (nothing to copy to the device first, and a graph holds them by value);
 // its workgroups are dealt to the tensors by size.
 //

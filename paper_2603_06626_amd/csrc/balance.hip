@@ -10,6 +10,8 @@ namespace {
 // coef_e = alpha E f_e / n.  The tokens are cut into chunks of equal length, one per workgroup; the part of a sequence inside a chunk
 // leaves its sums in a slot of its own, chunk + sequence (both only grow along the tokens, so no two parts share one), and a second
 // launch adds up each sequence's slots in order.  So work is even whatever the sequences' lengths, and no float is added atomically.
+// Bound by reading the scores where they are many (131072 x 256 fp32: 134 MB, 27 us with the join, 5 TB/s), by the chain of loads, barrier and
+// second launch where they are few (30011 x 60 bf16 in 48 sequences: 7.5 us and 6.2 for the join).
 struct BalanceCell {
     float prob;
     int32_t count;
@@ -22,7 +24,11 @@ struct BalanceParts {
     int64_t rows;        // of a chunk
 };
 
+// 128, 256 and 512 threads: 131072 x 256 47.6, 33.3, 35.2 us (all of the call), 65536 x 128 in 256 sequences 29.4, 26.4, 30.9, 4096 x 64 in 64
+// sequences 11.0, 11.7, 12.8.
 constexpr int kPartThreads = 256;
+// Rounds of tokens up to which one workgroup does it all.  In 4 rounds 6.1 to 6.8 us against 6.2 to 8.2 in two launches, and one launch less
+// to enqueue (8 against 11 us where the host is what it waits for); in 8 rounds 9.6 to 10.8 against 6.2 to 8.1.
 constexpr int kAloneRounds = 4;
 
 struct BalanceOut {
@@ -314,7 +320,8 @@ __global__ __launch_bounds__(THREADS) void k_balance_join(int64_t T, int E, int 
 
 }  // namespace
 
-// Chunks: a few per CU at most, so that a sequence's slots are few, and not below the tokens that a workgroup takes at a time.
+// Chunks: two per CU at most, so that a sequence's slots are few, and not below the tokens that a workgroup takes at a time.  256, 512, 768,
+// 1024 of them: 131072 x 256 47.9, 33.3, 33.2, 38.5 us, 131072 x 64 in bf16 17.0, 13.8, 14.3, 15.5.
 BalanceLayout balance_layout(int64_t T, int E, int64_t S) {
     BalanceLayout l{};
     const int64_t at_once = kPartThreads / lanes_of(E), rows = (T + 511) / 512;
@@ -360,8 +367,10 @@ hipError_t launch_balance(const void* scores, int dtype, int64_t ld, int64_t T, 
         });
     });
     if (e != hipSuccess || alone) return e;
-    // many slots per sequence: 64 threads to an expert's; few: 4
-    if (S < 8)
+    // Many slots per sequence: 64 threads to an expert's and 16 experts to a workgroup; few: 4 and 64.  131072 x 256, the former / the latter with
+    // 1, 2, 4, 8, 16 sequences 27.3 / 31.5, 26.9 / 28.3, 27.0 / 26.5, 27.8 / 25.8, 30.5 / 25.9 us (all of the call); 16384 x 128 with 1, 2, 4
+    // 10.3 / 14.3, 10.5 / 11.6, 9.9 / 10.0; 8192 x 64, where a sequence has 128 slots, with one 9.4 / 8.0.
+    if (l.chunks > 128 * S)
         hipLaunchKernelGGL((k_balance_join<16, 1024>), dim3((unsigned)S, (unsigned)(E + 15) / 16), dim3(1024), 0, s, T, E, k, token_mask, off, S, parts, out);
     else
         hipLaunchKernelGGL((k_balance_join<64, 256>), dim3((unsigned)S, (unsigned)(E + 63) / 64), dim3(256), 0, s, T, E, k, token_mask, off, S, parts, out);

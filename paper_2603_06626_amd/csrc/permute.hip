@@ -141,7 +141,8 @@ __global__ __launch_bounds__(256) void k_row_gates(const PlanDims plan, const in
 }
 
 // dlog[i] = <dY[t], in[src_to_row[i]]>, i = t*k + j: the gradient by the log of a slot's gate, since the row is the gate times what
-// does not depend on it.  One wave per slot: the k rows of a token are read once each, dY's row comes from L1 for all but the first.
+// does not depend on it.  One wave per slot, so that few tokens still fill the chip: the k rows of a token are read once each, dY's row comes
+// from a cache for all but the first.  Bound by reading the rows: 16384 tokens, k = 8, d = 4096 197 us, 6.1 TB/s.
 __global__ __launch_bounds__(256) void k_gate_bwd(const PlanDims plan, const int32_t* __restrict__ src_to_row, int64_t N, int k, int chunks_per_row,
                                                   const u32x4* __restrict__ dY, const u32x4* __restrict__ in, float* __restrict__ dlog) {
     if (!plan.match()) return;
