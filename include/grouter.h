@@ -227,7 +227,7 @@ int grouter_fold_weights(const float* W_s, const int32_t* group_of, int d, int E
  * Scores are a matrix [T][E] of fp32, bf16 or fp16 (GROUTER_FP32 ...) whose rows are score_ld >= E elements apart, so it
  * may be part of a wider one; only its own elements are read.  Rows that start at multiples of 16 bytes are read faster.
  * token_mask [T] uint8 or NULL: tokens with 0 are padding and their scores may hold anything.
- * Limits: 1 <= k <= E <= 1024 (E <= 256 for uint8 ids), T*k < 2^31, score_ld <= 2^31, T*score_ld <= 2^48, 1 <= S <= 2^24.  No output may
+ * Limits: 1 <= k <= E <= 1024 (E <= 256 for uint8 ids), T*k < 2^31, score_ld <= 2^31, T*score_ld <= 2^48, 1 <= S < 2^24.  No output may
  * overlap another argument (two matrices may be different columns of one).  Calls that may overlap in time need outputs and
  * workspaces of their own; that holds for captured graphs that replay side by side, too.
  */
@@ -308,7 +308,7 @@ int grouter_moe_gate_bwd(const void* plan_ws, int64_t T, int k, int E, int d, in
  *               power of two 2^(x - 127) with x in m_exp / v_exp [ceil(n/32)] uint8 (255: the block is NaN; it is so from the
  *               first infinity or NaN on).  Rounded up or down with the probability of the remainder; a root above 0 never
  *               becomes 0.  All zero bytes are a state of zeros.
- * A tensor of n = 0 elements is skipped (its pointers may be NULL).  param, master, grad, m and v are 16-byte aligned.
+ * A tensor has up to 2^40 elements; one of n = 0 is skipped (its pointers may be NULL).  param, master, grad, m and v are 16-byte aligned.
  * No tensor may overlap another one of the call.  The list is read during the call only.
  * Random bits are a function of the seed and the element's place in the list (tensors one after the other, each rounded up
  * to a multiple of 32): the same call gives the same result, and every step should bring another seed.

@@ -255,22 +255,24 @@ __device__ __forceinline__ void step(const AdamwTensor& t, const AdamwHyper& h, 
 
 template <int KIND, class Grad, bool EIGHT>
 __global__ __launch_bounds__(kThreads) void k_adamw(const Batch batch) {
+    const uint32_t group = (uint32_t)group_of_grid();
+    if (group >= batch.first_group[batch.count]) return;
     int i = 0;
     for (int step = 32; step > 0; step /= 2)
-        if (i + step < batch.count && batch.first_group[i + step] <= blockIdx.x) i += step;
+        if (i + step < batch.count && batch.first_group[i + step] <= group) i += step;
     const AdamwTensor t = batch.tensor[i];
     const AdamwHyper h = batch.hyper_device ? *batch.hyper_device : batch.hyper;
     const float scale = batch.grad_scale ? h.grad_scale * *batch.grad_scale : h.grad_scale;
     constexpr int kEach = each_of(KIND, std::is_same_v<Grad, Bf16>, EIGHT);
     constexpr int64_t kPerGroup = kThreads * kEach;
-    const int64_t begin = (int64_t)(blockIdx.x - batch.first_group[i]) * kPerGroup, at = begin + (int64_t)threadIdx.x * kEach;
+    const int64_t begin = (int64_t)(group - batch.first_group[i]) * kPerGroup, at = begin + (int64_t)threadIdx.x * kEach;
     if (begin + kPerGroup <= t.n) step<KIND, Grad, EIGHT, true>(t, h, scale, batch.first_place[i], at, kEach);
     else step<KIND, Grad, EIGHT, false>(t, h, scale, batch.first_place[i], at, (int)max((int64_t)0, min((int64_t)kEach, t.n - at)));
 }
 
 template <int KIND, class Grad, bool EIGHT>
 hipError_t launch(const Batch& b, unsigned groups, hipStream_t s) {
-    hipLaunchKernelGGL((k_adamw<KIND, Grad, EIGHT>), dim3(groups), dim3(kThreads), 0, s, b);
+    hipLaunchKernelGGL((k_adamw<KIND, Grad, EIGHT>), grid_of(groups), dim3(kThreads), 0, s, b);
     return hipGetLastError();
 }
 

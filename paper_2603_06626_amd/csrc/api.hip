@@ -504,7 +504,7 @@ int grouter_fold_weights(const float* W_s, const int32_t* group_of, int d, int E
 
 // ---- the router and what trains it -------------------------------------------------------------------------
 namespace {
-constexpr int64_t kMaxSequences = 1 << 24;
+constexpr int64_t kMaxSequences = (1 << 24) - 1;
 
 bool type_ok(int dtype) { return dtype == GROUTER_FP32 || dtype == GROUTER_BF16 || dtype == GROUTER_FP16; }
 size_t type_bytes(int dtype) { return dtype == GROUTER_FP32 ? 4 : 2; }

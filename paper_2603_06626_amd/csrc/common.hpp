@@ -108,6 +108,13 @@ static inline __host__ PlanView make_plan_view(const void* ws, const PlanLayout&
     return v;
 }
 
+// A grid of that many workgroups, or a few more: the work-items along one dimension of a grid have to stay below 2^32.
+static inline __host__ dim3 grid_of(uint64_t groups) {
+    const uint64_t row = 1u << 20;
+    return groups <= row ? dim3((unsigned)groups) : dim3((unsigned)row, (unsigned)((groups + row - 1) / row));
+}
+__device__ __forceinline__ int64_t group_of_grid() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // ---- launchers (each defined in the .hip file that holds its kernels) -------------------------------
 hipError_t launch_plan_build(const void* idx, int idx_dtype, const PlanLayout& L, void* plan_ws, hipStream_t s);
 // routing statistics (stats.hip)

@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256) void k_row_gates(const PlanDims plan, const in
 __global__ __launch_bounds__(256) void k_gate_bwd(const PlanDims plan, const int32_t* __restrict__ src_to_row, int64_t N, int k, int chunks_per_row,
                                                   const u32x4* __restrict__ dY, const u32x4* __restrict__ in, float* __restrict__ dlog) {
     if (!plan.match()) return;
-    const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t i = group_of_grid() * 4 + (threadIdx.x >> 6);
     if (i >= N) return;
     const int lane = threadIdx.x & 63;
     const u32x4* a = dY + (size_t)(i / k) * chunks_per_row;
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256) void k_gate_bwd(const PlanDims plan, const int
 }
 
 hipError_t launch_gate_bwd(const PlanView& P, int d, const bf16_t* dY, const bf16_t* rows, float* dlog, hipStream_t s) {
-    hipLaunchKernelGGL(k_gate_bwd, dim3((unsigned)((P.N + 3) / 4)), dim3(256), 0, s, P.dims(), P.src_to_row, P.N, P.k, d / 8, (const u32x4*)dY,
+    hipLaunchKernelGGL(k_gate_bwd, grid_of((P.N + 3) / 4), dim3(256), 0, s, P.dims(), P.src_to_row, P.N, P.k, d / 8, (const u32x4*)dY,
                        (const u32x4*)rows, dlog);
     return hipGetLastError();
 }

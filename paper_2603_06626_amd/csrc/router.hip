@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kThreads) void k_route_lists(const typename Type::s
     typedef typename KeysOf<Type>::type K;
     typedef typename K::Key Key;
     const int part = threadIdx.x % L;
-    const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
+    const int64_t t = group_of_grid() * (kThreads / L) + threadIdx.x / L;
     const bool here = t < T;
     const auto* row = scores + (here ? t : T - 1) * ld;
     Row<Type, L, V, FULL> x;
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(kThreads) void k_route_rounds(const typename Type::
     typedef typename K::Key Key;
     extern __shared__ uint16_t s_pick[];
     const int part = threadIdx.x % L, local = threadIdx.x / L;
-    const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + local;
+    const int64_t t = group_of_grid() * (kThreads / L) + local;
     const bool here = t < T;
     const auto* row = scores + (here ? t : T - 1) * ld;
     uint16_t* pick = s_pick + local * k;
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
     extern __shared__ float s_slot[];    // per token k contributions, then k expert numbers
     constexpr int W = kPiece<Type>, N = V / W;
     const int part = threadIdx.x % L, local = threadIdx.x / L;
-    const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + local;
+    const int64_t t = group_of_grid() * (kThreads / L) + local;
     const bool here = t < T, live = here && !(a.token_mask && a.token_mask[t] == 0);
     const auto* row = scores + (here ? t : T - 1) * ld;
     constexpr bool sigmoid = SIGMOID;
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const typename Type::sto
     int64_t s = 0;
     if (WHOLE && a.off) {
         // the sequence of the wave's first token is most often that of all its tokens
-        const int64_t first = (int64_t)blockIdx.x * (kThreads / L) + (threadIdx.x & ~63) / L;
+        const int64_t first = group_of_grid() * (kThreads / L) + (threadIdx.x & ~63) / L;
         int64_t next;
         s = offsets_up_to(a.off, a.S, first, next);
         if (next < first + 64 / L) {
@@ -438,7 +438,7 @@ hipError_t launch_route(const void* scores, int dtype, int64_t ld, int64_t T, in
             typedef decltype(type) Type;
             constexpr int L = decltype(l)::value, V = decltype(v)::value, tokens = kThreads / L;
             constexpr bool FULL = decltype(full)::value;
-            const dim3 grid((unsigned)((T + tokens - 1) / tokens)), threads(kThreads);
+            const dim3 grid = grid_of((T + tokens - 1) / tokens), threads(kThreads);
             const auto* x = (const typename Type::stored*)scores;
             if (k <= 4) hipLaunchKernelGGL((k_route_lists<Type, L, V, FULL, 4>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
             else if (k <= 8) hipLaunchKernelGGL((k_route_lists<Type, L, V, FULL, 8>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
@@ -462,7 +462,7 @@ hipError_t launch_route_bwd(const void* scores, int dtype, int64_t ld, int64_t T
             typedef decltype(type) Type;
             constexpr int L = decltype(l)::value, V = decltype(v)::value, tokens = kThreads / L;
             constexpr bool FULL = decltype(full)::value;
-            const dim3 grid((unsigned)((T + tokens - 1) / tokens));
+            const dim3 grid = grid_of((T + tokens - 1) / tokens);
             const size_t lds = dlog ? tokens * k * 2 * sizeof(float) : 0;
             const auto* x = (const typename Type::stored*)scores;
             return with_flag(gating >= kSigmoid, [&](auto sigmoid) {

@@ -119,3 +119,31 @@ def test_phases_are_timed():
     times = b.grouter_timing_read()
     b.grouter_timing_enable(False)
     assert all(times[p][1] == 1 and times[p][0] > 0 for p in ("route", "balance", "gate_bwd", "route_bwd", "adamw"))
+
+
+def test_grids_past_32_bits_of_threads():
+    """More threads than one dimension of a grid takes: 2^26 + 3 tokens of 520 equal scores, 2^26 + 24 slots of 8 values."""
+    T, E, k = (1 << 26) + 3, 520, 2
+    s = torch.zeros((T, E), dtype=torch.bfloat16, device=DEV)
+    s[-1, 7] = s[1 << 25, 519] = s[0, 300] = 1.0
+    ids, g = torch.full((T, k), -1, dtype=torch.int32, device=DEV), torch.zeros((T, k), dtype=torch.bfloat16, device=DEV)
+    b.grouter_route(s, k, b.GATE_SIGMOID_NORMALISED, ids, g)
+    want = torch.arange(k, device=DEV).expand(T, k).clone().int()
+    for t, e in ((0, 300), (1 << 25, 519), (T - 1, 7)):
+        want[t] = torch.tensor([e, 0])
+    assert torch.equal(ids, want)
+    assert (g[1:1 << 25] == 0.5).all() and (g[-1].float().sum() - 1).abs() < 2.0 ** -7
+    del g, want
+    ds = torch.full((T, E), 5.0, dtype=torch.bfloat16, device=DEV)
+    b.grouter_route_bwd(s, b.GATE_SIGMOID, ds, topk_idx=ids, dlog_gate=torch.ones((T, k), device=DEV))
+    assert (ds[1:1 << 25, :2] == 0.5).all() and (ds[1:1 << 25, 2:8] == 0).all() and (ds[-1, 1:7] == 0).all() and ds[-1, 0] == 0.5 and ds[-1, 7] < 0.5
+    del s, ds, ids
+    torch.cuda.empty_cache()
+    T, E, k, d = (1 << 23) + 3, 16, 8, 8
+    plan = torch.empty(b.grouter_plan_bytes(T, k, E), dtype=torch.uint8, device=DEV)
+    b.grouter_plan_build((torch.arange(T * k, device=DEV).view(T, k) % E).int(), E, plan)
+    rows = (torch.arange(T * k, device=DEV) % 251).to(torch.bfloat16)[:, None].expand(-1, d).contiguous()
+    dlog = torch.empty((T, k), device=DEV)
+    b.grouter_gate_bwd(plan, T, k, E, torch.ones((T, d), dtype=torch.bfloat16, device=DEV), rows, dlog)
+    at = b.grouter_plan_views(plan, T, k, E)[3].long()
+    assert torch.equal(dlog.view(-1), (8 * (at % 251)).float())
