@@ -82,22 +82,29 @@ __device__ __forceinline__ float power_of_two(int biased) {   // 2^(biased - 127
     return __uint_as_float(biased == 255 ? 0x7fc00000u : biased == 0 ? 0x00400000u : (uint32_t)biased << 23);
 }
 // e4m3 codes of x >= 0 times 2^(127 - exp); up: 20 random bits each.  Numbers below 2^-6 (less than a 28000th of the block's largest) have
-// codes in equal steps, and blocks that are not finite one code for all: both are looked at only where a wave has some.
-template <int N>
-__device__ __forceinline__ void codes_of(const float (&x)[N], int exp, const uint32_t (&up)[N], uint32_t (&code)[N]) {
+// codes in equal steps, and blocks that are not finite one code for all: both are looked at only where a wave has some.  ROOT: x is the
+// hardware's root of v, off by up to one unit; where that could make another code (two of 2^20 random numbers), the root is taken
+// again, rounded to nearest, so that the code is that of the formula on every machine.
+template <bool ROOT, int N>
+__device__ __forceinline__ void codes_of(const float (&x)[N], const float (&v)[N], int exp, const uint32_t (&up)[N], uint32_t (&code)[N]) {
     const float scale = power_of_two(254 - exp);
     float y[N], least = INFINITY;
+    uint32_t nearest = 2;     // how near a sum's low bits come to the next code, from either side
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         y[j] = x[j] * scale;
         least = fminf(least, y[j]);
-        code[j] = min(((__float_as_uint(y[j]) + up[j]) >> 20) - 960u, 126u);
+        const uint32_t sum = __float_as_uint(y[j]) + up[j];
+        if (ROOT) nearest = min(nearest, (sum + 1) & 0xfffffu);
+        code[j] = min((sum >> 20) - 960u, 126u);
     }
-    if (__ballot(least < 0x1p-6f || exp == 255)) {
+    if (__ballot(least < 0x1p-6f || exp == 255 || (ROOT && nearest < 2))) {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
+            if (ROOT) y[j] = (float)__builtin_sqrt((double)v[j]) * scale;
+            const uint32_t normal = min(((__float_as_uint(y[j]) + up[j]) >> 20) - 960u, 126u);
             const uint32_t small = (uint32_t)(y[j] * 512.f + (float)up[j] * 0x1p-20f);
-            code[j] = exp == 255 ? 127u : y[j] < 0x1p-6f ? small : code[j];
+            code[j] = exp == 255 ? 127u : y[j] < 0x1p-6f ? small : normal;
         }
     }
 }
@@ -235,13 +242,13 @@ __device__ __forceinline__ void step(const AdamwTensor& t, const AdamwHyper& h, 
             size[j] = fabsf(m[j]);
             up[j] = noise[j] >> 12;
         }
-        codes_of(size, em, up, code);
+        codes_of<false>(size, size, em, up, code);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             cm[j] = (uint8_t)(code[j] | (__float_as_uint(m[j]) >> 31 << 7));
             up[j] = (noise[j] & 0xfffu) << 8 | 128u;
         }
-        codes_of(root, ev, up, code);
+        codes_of<true>(root, v, ev, up, code);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) cv[j] = (uint8_t)(v[j] > 0.f ? max(code[j], 1u) : code[j]);
         put<kEach, WHOLE>((uint8_t*)t.m, at, n, cm);

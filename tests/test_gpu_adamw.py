@@ -233,6 +233,43 @@ def test_moments_in_8_bits_follow_those_in_32():
     assert 0.9 * exact < root.mean() < 1.7 * exact
 
 
+def codes_in_fp32(x, exps, up, least):
+    """The codes of x >= 0 (fp32) as the format defines them, in fp32 and whole numbers."""
+    y = x * np.repeat(2.0 ** (127.0 - exps), 32).astype(np.float32)[:len(x)]
+    normal = ((y.view(np.uint32).astype(np.int64) + up) >> 20) - 960
+    small = np.floor(y * np.float32(512) + up.astype(np.float32) * np.float32(2.0 ** -20)).astype(np.int64)
+    code = np.minimum(np.where(y < 2.0 ** -6, small, normal), 126)
+    return np.where((y > 0) & (code < least), least, code)
+
+
+@pytest.mark.parametrize("spread", [0.0, 4.0])
+def test_codes_are_those_of_the_formulas_bit_for_bit(spread):
+    """Moments in fp32 with every product and sum rounded, roots rounded to nearest: the 8-bit states of millions of elements follow exactly,
+    also where gradients span many binades and codes lie in equal steps."""
+    n, f = 2_000_032, np.float32
+    rng = np.random.default_rng(int(spread))
+    kw = dict(m_exp=[torch.zeros(n // 32, dtype=torch.uint8, device=DEV)], v_exp=[torch.zeros(n // 32, dtype=torch.uint8, device=DEV)])
+    m, v = (torch.zeros(n, dtype=torch.uint8, device=DEV) for _ in range(2))
+    grad = torch.zeros(n, device=DEV)
+    t = b.AdamWTensors([torch.zeros(n, device=DEV)], [grad], [m], [v], **kw)
+    em, ev, cm, cv = np.zeros(n // 32, np.int64), np.zeros(n // 32, np.int64), np.zeros(n, np.int64), np.zeros(n, np.int64)
+    for step in range(1, 5):
+        g = (rng.normal(size=n) * np.exp(spread * rng.normal(size=n)) * 1e-3).astype(f)
+        grad.copy_(torch.from_numpy(g))
+        b.grouter_adamw(t, b.grouter_adamw_hyper(step=step, seed=step, **HYPER))
+        value = o.E4M3.astype(f)
+        sm, sv = (np.repeat(2.0 ** (e - 127.0), 32).astype(f) for e in (em, ev))
+        old = value[cv] * sv
+        fm = (value[cm] * sm) * f(0.9) + g * f(1 - 0.9)
+        fv = (old * old) * f(0.99) + (g * g) * f(1 - 0.99)
+        em, ev = o.shared_exponents(np.abs(fm).astype(np.float64)), o.shared_exponents(np.sqrt(fv.astype(np.float64)))
+        h = o.noise(np.arange(n, dtype=np.uint64), step).astype(np.int64)
+        cm = codes_in_fp32(np.abs(fm), em, h >> 12, 0) + 128 * np.signbit(fm)
+        cv = codes_in_fp32(np.sqrt(fv.astype(np.float64)).astype(f), ev, (h & 0xfff) * 256 + 128, 1)
+        for got, want in ((kw["m_exp"][0], em), (kw["v_exp"][0], ev), (m, cm), (v, cv)):
+            assert np.array_equal(got.cpu().numpy().astype(np.int64), want), step
+
+
 def test_steps_in_a_graph_replay_with_the_buffers_contents():
     c, e = Case(SIZES, "bf16", "bf16", 8), Case(SIZES, "bf16", "bf16", 8)
     hyper = torch.zeros(48, dtype=torch.uint8, device=DEV)
