@@ -252,7 +252,8 @@ __global__ __launch_bounds__(THREADS) void k_balance_join(int64_t T, int E, int 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t s = blockIdx.x;
     const int64_t begin = off ? max((int64_t)0, off[s]) : 0, end = off ? min(T, off[s + 1]) : T;
-    const int64_t c0 = begin / parts.rows, c1 = begin < end ? (end - 1) / parts.rows + 1 : c0;
+    const uint32_t rows = (uint32_t)parts.rows;      // as all of begin, end: at most T
+    const int64_t c0 = begin < end ? (uint32_t)begin / rows : 0, c1 = begin < end ? (uint32_t)(end - 1) / rows + 1 : 0;
     const int col = threadIdx.x % COLUMNS, e = blockIdx.y * COLUMNS + col;
     double sum = 0.0;
     int count = 0, tokens = 0;

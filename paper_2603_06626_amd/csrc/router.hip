@@ -440,14 +440,20 @@ hipError_t launch_route(const void* scores, int dtype, int64_t ld, int64_t T, in
             constexpr bool FULL = decltype(full)::value;
             const dim3 grid = grid_of((T + tokens - 1) / tokens), threads(kThreads);
             const auto* x = (const typename Type::stored*)scores;
-            if (k <= 4) hipLaunchKernelGGL((k_route_lists<Type, L, V, FULL, 4>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
-            else if (k <= 8) hipLaunchKernelGGL((k_route_lists<Type, L, V, FULL, 8>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
-            else if (V == 16 && k <= 16 && (dtype == 0 || E <= 256 || k > 12)) {
+            if (k <= 4) {
+                hipLaunchKernelGGL((k_route_lists<Type, L, V, FULL, 4>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
+            } else if (k <= 8) {
+                hipLaunchKernelGGL((k_route_lists<Type, L, V, FULL, 8>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
+            } else if constexpr (V == 16) {     // (more than 8 experts)
                 // Lists of 16 cost the same for 9 and for 16 experts, rounds grow with k (262144 tokens; rounds / lists in us): E = 128, k = 10
                 // 38 / 35 with bf16 and 71 / 49 with fp32 scores, k = 16 52 / 35 and 98 / 49; bf16, E = 256 73 / 76 and 98 / 75; a quarter of
                 // the tokens with E = 512 37 / 43 and 52 / 43, with E = 1024 74 / 92 and 100 / 91; fp32, E = 1024 138 / 131 and 200 / 127.
-                if constexpr (V == 16) hipLaunchKernelGGL((k_route_lists<Type, L, V, FULL, 16>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
-            } else hipLaunchKernelGGL((k_route_rounds<Type, L, V, FULL>), grid, threads, tokens * k * sizeof(uint16_t), s, x, ld, T, E, k, gating, token_mask, out);
+                if (k <= 16 && (dtype == 0 || E <= 256 || k > 12))
+                    hipLaunchKernelGGL((k_route_lists<Type, L, V, FULL, 16>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
+                else
+                    hipLaunchKernelGGL((k_route_rounds<Type, L, V, FULL>), grid, threads, tokens * k * sizeof(uint16_t), s, x, ld, T, E, k, gating,
+                                       token_mask, out);
+            }
             return hipGetLastError();
         });
     });
