@@ -505,18 +505,29 @@ def _sequences(seq_offsets):
     return seq_offsets.data_ptr(), seq_offsets.numel() - 1
 
 
+def _address(t, name, dtype, shape):
+    """The address of a contiguous GPU tensor of that type and shape."""
+    if not (t.is_cuda and t.is_contiguous()) or t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name} must be a contiguous GPU tensor of {dtype} {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _ids(topk_idx, T, k):
+    """The address and the type of expert ids [T,k]."""
+    kind = _idx_dtype(topk_idx)
+    return _address(topk_idx, "topk_idx", topk_idx.dtype, (T, k)), kind
+
+
 def grouter_route(scores, k, gating, topk_idx, gate_w, token_mask=None, stream=None):
     """scores [T,E] fp32/bf16/fp16 (rows may be apart); topk_idx [T,k] int32/uint8 and gate_w [T,k] bf16 are written."""
     import torch
 
     ld = _matrix(scores, "scores")
     T, E = scores.shape
-    _dev(topk_idx, "topk_idx")
-    _dev(gate_w, "gate_w", torch.bfloat16)
-    if topk_idx.shape != (T, k) or gate_w.shape != (T, k):
-        raise ValueError("shape mismatch")
-    _check(lib().grouter_route(_p(scores), _float_dtype(scores, "scores"), ld, T, E, k, gating, _mask(token_mask, T), _p(topk_idx),
-                               _idx_dtype(topk_idx), _p(gate_w), _stream_for(scores, stream)), "grouter_route")
+    ids, kind = _ids(topk_idx, T, k)
+    gates = _address(gate_w, "gate_w", torch.bfloat16, (T, k))
+    _check(lib().grouter_route(scores.data_ptr(), _float_dtype(scores, "scores"), ld, T, E, k, gating, _mask(token_mask, T), ids, kind, gates,
+                               _stream_for(scores, stream)), "grouter_route")
 
 
 def grouter_route_bwd(scores, gating, dscores, topk_idx=None, dlog_gate=None, token_mask=None, seq_offsets=None, coef=None, stream=None):
@@ -524,20 +535,20 @@ def grouter_route_bwd(scores, gating, dscores, topk_idx=None, dlog_gate=None, to
     import torch
 
     ld, dld = _matrix(scores, "scores"), _matrix(dscores, "dscores")
-    T, E = scores.shape
-    off, S = _sequences(seq_offsets) if coef is not None else (None, 1)
-    k = it = 0
-    if dlog_gate is not None:
-        _dev(dlog_gate, "dlog_gate", torch.float32)
-        _dev(topk_idx, "topk_idx")
-        k, it = topk_idx.shape[1], _idx_dtype(topk_idx)
-        if topk_idx.shape != (T, k) or dlog_gate.shape != (T, k):
-            raise ValueError("shape mismatch")
-    if coef is not None and _dev(coef, "coef", torch.float32).shape != (S, E) or dscores.shape != (T, E):
+    T, E = shape = scores.shape
+    if dscores.shape != shape:
         raise ValueError("shape mismatch")
-    _check(lib().grouter_route_bwd(_p(scores), _float_dtype(scores, "scores"), ld, T, E, gating, _mask(token_mask, T),
-                                   _p(topk_idx) if k else None, it, k, _p(dlog_gate), off, S, _p(coef), _p(dscores),
-                                   _float_dtype(dscores, "dscores"), dld, _stream_for(scores, stream)), "grouter_route_bwd")
+    off = ids = dlog = weights = None
+    S, k, kind = 1, 0, 0
+    if coef is not None:
+        off, S = _sequences(seq_offsets)
+        weights = _address(coef, "coef", torch.float32, (S, E))
+    if dlog_gate is not None:
+        k = dlog_gate.shape[-1]
+        ids, kind = _ids(topk_idx, T, k)
+        dlog = _address(dlog_gate, "dlog_gate", torch.float32, (T, k))
+    _check(lib().grouter_route_bwd(scores.data_ptr(), _float_dtype(scores, "scores"), ld, T, E, gating, _mask(token_mask, T), ids, kind, k, dlog, off, S,
+                                   weights, dscores.data_ptr(), _float_dtype(dscores, "dscores"), dld, _stream_for(scores, stream)), "grouter_route_bwd")
 
 
 def grouter_balance_bytes(T, E, S) -> int:
@@ -551,15 +562,14 @@ def grouter_balance(scores, gating, topk_idx, alpha, counts, prob, coef, loss, w
     ld = _matrix(scores, "scores")
     T, E = scores.shape
     off, S = _sequences(seq_offsets)
-    _dev(topk_idx, "topk_idx")
-    _dev(counts, "counts", torch.int32)
-    for t, n in ((prob, "prob"), (coef, "coef"), (loss, "loss")):
-        _dev(t, n, torch.float32)
-    k = topk_idx.shape[1]
-    if topk_idx.shape != (T, k) or counts.shape != (S, E) or prob.shape != (S, E) or coef.shape != (S, E) or loss.numel() != 1:
-        raise ValueError("shape mismatch")
-    _check(lib().grouter_balance(_p(scores), _float_dtype(scores, "scores"), ld, T, E, k, gating, _mask(token_mask, T), _p(topk_idx),
-                                 _idx_dtype(topk_idx), off, S, alpha, _p(counts), _p(prob), _p(coef), _p(loss), _p(_dev(ws, "ws")),
+    k = topk_idx.shape[-1]
+    ids, kind = _ids(topk_idx, T, k)
+    fp32, per_sequence = torch.float32, (S, E)
+    if not loss.numel() == 1:
+        raise ValueError("loss must have one element")
+    _check(lib().grouter_balance(scores.data_ptr(), _float_dtype(scores, "scores"), ld, T, E, k, gating, _mask(token_mask, T), ids, kind, off, S, alpha,
+                                 _address(counts, "counts", torch.int32, per_sequence), _address(prob, "prob", fp32, per_sequence),
+                                 _address(coef, "coef", fp32, per_sequence), _dev(loss, "loss", fp32).data_ptr(), _dev(ws, "ws").data_ptr(),
                                  ws.numel() * ws.element_size(), _stream_for(scores, stream)), "grouter_balance")
 
 
@@ -567,29 +577,23 @@ def grouter_gate_bwd(plan_ws, T, k, E, dY, inp, dlog_gate, stream=None):
     """dlog_gate fp32 [T,k] from dY bf16 [T,d] and rows inp bf16 [T*k,d] in expert-sorted order."""
     import torch
 
-    _dev(plan_ws, "plan_ws")
-    for t, n in ((dY, "dY"), (inp, "in")):
-        _dev(t, n, torch.bfloat16)
-    _dev(dlog_gate, "dlog_gate", torch.float32)
-    d = dY.shape[1]
-    if dY.shape != (T, d) or inp.shape != (T * k, d) or dlog_gate.shape != (T, k) or plan_ws.numel() < grouter_plan_bytes(T, k, E):
-        raise ValueError("shape mismatch")
-    _check(lib().grouter_gate_bwd(_p(plan_ws), T, k, E, d, _p(dY), _p(inp), _p(dlog_gate), _stream_for(dY, stream)), "grouter_gate_bwd")
+    bf, d = torch.bfloat16, dY.shape[-1]
+    if _dev(plan_ws, "plan_ws").numel() < grouter_plan_bytes(T, k, E):
+        raise ValueError("plan_ws is smaller than a plan of this size")
+    _check(lib().grouter_gate_bwd(plan_ws.data_ptr(), T, k, E, d, _address(dY, "dY", bf, (T, d)), _address(inp, "in", bf, (T * k, d)),
+                                  _address(dlog_gate, "dlog_gate", torch.float32, (T, k)), _stream_for(dY, stream)), "grouter_gate_bwd")
 
 
 def grouter_moe_gate_bwd(plan_ws, E, f, dY, ctx_ws, dlog_gate, stream=None):
     """The same on the rows that grouter_moe_fwd kept in ctx_ws."""
     import torch
 
-    _dev(plan_ws, "plan_ws")
-    _dev(dY, "dY", torch.bfloat16)
-    _dev(ctx_ws, "ctx_ws")
-    _dev(dlog_gate, "dlog_gate", torch.float32)
     T, k = dlog_gate.shape
-    d = dY.shape[1]
-    if dY.shape != (T, d) or plan_ws.numel() < grouter_plan_bytes(T, k, E):
-        raise ValueError("shape mismatch")
-    _check(lib().grouter_moe_gate_bwd(_p(plan_ws), T, k, E, d, f, _p(dY), _p(ctx_ws), ctx_ws.numel(), _p(dlog_gate), _stream_for(dY, stream)),
+    d = dY.shape[-1]
+    if _dev(plan_ws, "plan_ws").numel() < grouter_plan_bytes(T, k, E):
+        raise ValueError("plan_ws is smaller than a plan of this size")
+    _check(lib().grouter_moe_gate_bwd(plan_ws.data_ptr(), T, k, E, d, f, _address(dY, "dY", torch.bfloat16, (T, d)), _dev(ctx_ws, "ctx_ws").data_ptr(),
+                                      ctx_ws.numel(), _address(dlog_gate, "dlog_gate", torch.float32, (T, k)), _stream_for(dY, stream)),
            "grouter_moe_gate_bwd")
 
 
