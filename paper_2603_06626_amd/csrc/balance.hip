@@ -10,7 +10,7 @@ namespace {
 // coef_e = alpha E f_e / n.  The tokens are cut into chunks of equal length, one per workgroup; the part of a sequence inside a chunk
 // leaves its sums in a slot of its own, chunk + sequence (both only grow along the tokens, so no two parts share one), and a second
 // launch adds up each sequence's slots in order.  So work is even whatever the sequences' lengths, and no float is added atomically.
-// Bound by reading the scores where they are many (131072 x 256 fp32: 134 MB, 27 us with the join, 5 TB/s), by the chain of loads, barrier and
+// Bound by reading where fp32 scores are many (131072 x 256: 27 us, 5 TB/s, and 6 for the join), by exponentials with bf16 ones (21), by the chain of loads, barrier and
 // second launch where they are few (30011 x 60 bf16 in 48 sequences: 7.5 us and 6.2 for the join).
 struct BalanceCell {
     float prob;
@@ -368,7 +368,7 @@ hipError_t launch_balance(const void* scores, int dtype, int64_t ld, int64_t T, 
         });
     });
     if (e != hipSuccess || alone) return e;
-    // Many slots per sequence: 64 threads to an expert's and 16 experts to a workgroup; few: 4 and 64.  131072 x 256, the former / the latter with
+    // Many slots per sequence: 64 threads to an expert's and 16 experts to a workgroup; few: 4 and 64.  131072 x 256 in bf16, the former / the latter with
     // 1, 2, 4, 8, 16 sequences 27.3 / 31.5, 26.9 / 28.3, 27.0 / 26.5, 27.8 / 25.8, 30.5 / 25.9 us (all of the call); 16384 x 128 with 1, 2, 4
     // 10.3 / 14.3, 10.5 / 11.6, 9.9 / 10.0; 8192 x 64, where a sequence has 128 slots, with one 9.4 / 8.0.
     if (l.chunks > 128 * S)
