@@ -97,8 +97,9 @@ __device__ __forceinline__ int64_t offsets_up_to(const int64_t* __restrict__ off
 }
 
 // What the probabilities over all experts of a row are shares of, softmax or sigmoids, for all that a lane fetched (an absent element has
-// the value that it has where it is present, and is left out of the sum).  Returns what they are to be multiplied with.  The shift goes into the product with log2 e as a fused sum: its rounding is
-// the same for all of a row, so no share depends on it.
+// the value that it has where it is present, and is left out of the sum).  Returns what they are to be multiplied with.  The row's largest
+// is subtracted before the product with log2 e: a product of its own would round by up to 2^-24 of a score that may be anything (an expert closed
+// by the type's lowest value, in a row of nothing else), and that error would be an exponent.
 template <bool SIGMOID, class Type, int L, int V, bool FULL>
 __device__ __forceinline__ float shares(const Row<Type, L, V, FULL>& x, float (&share)[V]) {
     float top = -INFINITY, z = 0.f;
@@ -115,9 +116,9 @@ __device__ __forceinline__ float shares(const Row<Type, L, V, FULL>& x, float (&
 #pragma unroll
         for (int v = 0; v < V; ++v) share[v] = sigmoid_of(share[v], top);
     } else {
-        top = shift_of(top) * 1.44269504f;
+        top = shift_of(top);
 #pragma unroll
-        for (int v = 0; v < V; ++v) share[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(share[v], 1.44269504f, -top));
+        for (int v = 0; v < V; ++v) share[v] = exp_of(share[v] - top);
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) z += x.has(v / x.W, v % x.W) ? share[v] : 0.f;
