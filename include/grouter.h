@@ -306,12 +306,15 @@ int grouter_moe_gate_bwd(const void* plan_ws, int64_t T, int k, int E, int d, in
  *   grad_dtype  GROUTER_FP32 or GROUTER_BF16
  *   state_bits  32: m, v are fp32.  8: m holds m and v holds sqrt(v) as e4m3 numbers (1 byte), each 32 neighbours under one
  *               power of two 2^(x - 127) with x in m_exp / v_exp [ceil(n/32)] uint8 (255: the block is NaN; it is so from the
- *               first infinity or NaN on).  Rounded up or down with the probability of the remainder; a root above 0 never
- *               becomes 0.  All zero bytes are a state of zeros.
+ *               first infinity or NaN on).  Rounded up or down with the probability of the remainder: exactly for m, and for
+ *               sqrt(v) where 1 - beta2 < 2^-10; up to there to the nearest of 4096 probabilities, which changes the rate at
+ *               which v decays by up to 1/32 of itself.  So sqrt(v) has the mean it should have, and v itself is higher by the
+ *               roundings' variance (a few per cent).  A root above 0 never becomes 0.  All zero bytes are a state of zeros.
  * A tensor has up to 2^40 elements; one of n = 0 is skipped (its pointers may be NULL).  param, master, grad, m and v are 16-byte aligned.
  * No tensor may overlap another one of the call.  The list is read during the call only.
  * Random bits are a function of the seed and the element's place in the list (tensors one after the other, each rounded up
- * to a multiple of 32): the same call gives the same result, and every step should bring another seed.
+ * to a multiple of 32): the same call gives the same result, and every step should bring another seed.  An element's 8-bit m and its
+ * BF16 parameter are rounded by the same bits, its root by others.
  *   hyper / hyper_dev  exactly one is given: the host's, taken by value, or one in device memory, read when the step runs (a
  *               captured step replays with what the buffer then holds).
  *   grad_scale_dev     NULL, or one fp32 on the device that multiplies grad_scale (a clipping coefficient, 1/loss scale)

@@ -143,6 +143,13 @@ def noise(places, seed):
     return h ^ (h >> np.uint64(16))
 
 
+def root_bits(words, beta2):
+    """The 20 random bits that round sqrt(v): a word's lower 12 and a half, or 8 bits more where 1 - beta2 < 2^-10."""
+    h = np.asarray(words, dtype=np.uint64)
+    more = (h * np.uint64(0x85EBCA6D) & np.uint64(0xffffffff)) >> np.uint64(24) if np.float32(1.0 - beta2) < 2.0 ** -10 else np.uint64(128)
+    return ((h & np.uint64(0xfff)) << np.uint64(8) | more).astype(np.int64)
+
+
 def places_of(sizes):
     """The places of every tensor's elements: tensors one after the other, each rounded up to a multiple of 32."""
     at, out = 0, []

@@ -11,7 +11,8 @@
 // neighbours, the smallest under which the largest is at most 448.  A root spans in 8 bits what v would need 16 binades more for.
 // Both are rounded up or down with the probability of the remainder: v changes by a thousandth per step at b2 = 0.999, which rounding to
 // nearest would throw away every time.  A root above zero never becomes zero (a step divided by eps alone would follow), a block with an
-// infinity or NaN becomes NaN as a whole.  The random bits are a function of the element's number and the seed.
+// infinity or NaN becomes NaN as a whole.  The random bits are a function of the element's number and the seed: of a word's 32, m takes the
+// upper 20 (all that a remainder has), the root the lower 12 and what kFineBelow says, a bf16 parameter the upper 16, which are m's too.
 //
 // The moments are computed with separately rounded products and sums (no fused multiply-add), so that their codes follow from the
 // formulas alone.
@@ -60,6 +61,13 @@ __device__ __forceinline__ uint32_t noise_of(uint32_t h) {
     h *= 0x7B1D4E65u;
     return h ^ (h >> 16);
 }
+
+// A root without gradients decays by (1 - beta2)/2 of itself per step, 8 to 16 times that of a code: at beta2 = 1 - 2^-10 16 of 4096 at
+// least, so that the word's lower 12 bits and a half of one keep the rate to 1/32 of it.  Closer to 1 the remainder is below that
+// resolution (0.9999: rates up to a fifth off, 0.99999: codes never move); there the word's product with an odd number gives 8 bits in the
+// half's place, which for every value of the 12 take all values equally often.  554 M elements in bf16 with 8-bit moments 1044 us,
+// 1038 without the choice, 1060 where the bits are taken.
+constexpr float kFineBelow = 0x1p-10f;
 
 // sqrt(v) to 1 unit; the hardware's takes what is below 2^-126 for 0, so where a wave holds such numbers (zeros mostly) all go the longer way
 template <int N>
@@ -247,6 +255,10 @@ __device__ __forceinline__ void step(const AdamwTensor& t, const AdamwHyper& h, 
         for (int j = 0; j < kEach; ++j) {
             cm[j] = (uint8_t)(code[j] | (__float_as_uint(m[j]) >> 31 << 7));
             up[j] = (noise[j] & 0xfffu) << 8 | 128u;
+        }
+        if (h.one_minus_beta2 < kFineBelow) {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) up[j] = (up[j] & ~0xffu) | noise[j] * 0x85EBCA6Du >> 24;
         }
         codes_of<true>(root, v, ev, up, code);
 #pragma unroll
