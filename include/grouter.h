@@ -340,7 +340,8 @@ typedef struct {
     uint32_t seed;
     uint32_t reserved[2];
 } grouter_adamw_hyper;
-/* Fills `out` (host) for step t = 1, 2, ...: 0 <= beta1, beta2 < 1, eps > 0, finite lr, weight_decay and grad_scale. */
+/* Fills `out` (host) for step t = 1, 2, ...: 0 <= beta1, beta2 < 1, finite lr and weight_decay; and as fp32 numbers, which is what the
+ * step computes with, eps at least 2^-126, the betas below 1, eps, lr/(1 - beta1^t), lr * weight_decay and grad_scale finite. */
 int grouter_adamw_hyper_set(double lr, double beta1, double beta2, double eps, double weight_decay, int64_t step,
                             double grad_scale, uint32_t seed, grouter_adamw_hyper* out);
 int grouter_adamw(const grouter_adamw_tensor* tensors, int count, int param_kind, int grad_dtype, int state_bits,

@@ -1,6 +1,7 @@
 // C ABI of the grouter library (see include/grouter.h): argument checks, workspace carving, launch order.
 #include "../../include/grouter.h"
 
+#include <cfloat>
 #include <cmath>
 #include <mutex>
 #include <vector>
@@ -600,20 +601,24 @@ int grouter_moe_gate_bwd(const void* plan_ws, int64_t T, int k, int E, int d, in
 
 int grouter_adamw_hyper_set(double lr, double beta1, double beta2, double eps, double weight_decay, int64_t step, double grad_scale,
                             uint32_t seed, grouter_adamw_hyper* out) {
-    if (!out || step < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps > 0.0) || !std::isfinite(eps) ||
-        !std::isfinite(lr) || !std::isfinite(weight_decay) || !std::isfinite(grad_scale))
+    if (!out || step < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return GROUTER_ERR_INVALID_ARG;
+    grouter_adamw_hyper h{};
+    h.beta1 = (float)beta1;
+    h.one_minus_beta1 = (float)(1.0 - beta1);
+    h.beta2 = (float)beta2;
+    h.one_minus_beta2 = (float)(1.0 - beta2);
+    h.inv_root_correction = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
+    h.eps = (float)eps;
+    h.step_size = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
+    h.decay = (float)(lr * weight_decay);
+    h.grad_scale = (float)grad_scale;
+    h.seed = seed;
+    // What the step computes with are these fp32 numbers: an eps below the smallest normal one has no reciprocal there (a weight whose moments
+    // are 0 would become NaN), a beta that rounds to 1 forgets nothing, and a product may leave the range that its factors are in.
+    if (!(h.eps >= FLT_MIN) || !std::isfinite(h.eps) || !(h.beta1 < 1.f) || !(h.beta2 < 1.f) || !std::isfinite(h.step_size) || !std::isfinite(h.decay) ||
+        !std::isfinite(h.grad_scale) || !std::isfinite(lr) || !std::isfinite(weight_decay))
         return GROUTER_ERR_INVALID_ARG;
-    *out = grouter_adamw_hyper{};
-    out->beta1 = (float)beta1;
-    out->one_minus_beta1 = (float)(1.0 - beta1);
-    out->beta2 = (float)beta2;
-    out->one_minus_beta2 = (float)(1.0 - beta2);
-    out->inv_root_correction = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
-    out->eps = (float)eps;
-    out->step_size = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
-    out->decay = (float)(lr * weight_decay);
-    out->grad_scale = (float)grad_scale;
-    out->seed = seed;
+    *out = h;
     return GROUTER_OK;
 }
 
