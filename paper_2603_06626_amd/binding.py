@@ -469,9 +469,9 @@ def _float_dtype(t, name, allowed=(FP32, BF16, FP16)):
     return dt
 
 
-def _matrix(t, name):
+def _matrix(t, name, at=None):
     """How far apart the rows of a GPU matrix are; a row is contiguous, its neighbours may be further off than its width."""
-    if t.is_cuda and t.dim() == 2:
+    if (t.is_cuda if at is None else t.get_device() == at) and t.dim() == 2:
         E = t.shape[1]
         if t.is_contiguous():
             return E
@@ -480,42 +480,62 @@ def _matrix(t, name):
             return rows
         if E == 1 and rows >= 1:
             return rows
-    raise ValueError(f"{name} must be a GPU matrix with contiguous rows")
+    raise ValueError(f"{name} must be a matrix with contiguous rows on {_place(at)}")
 
 
-def _mask(token_mask, T):
+def _place(at):
+    return "the GPU" if at is None else f"device {at}, as the call's other tensors"
+
+
+def _beside(t, name, at, dtype=None):
+    """A contiguous tensor on device `at` (None: any GPU), which a CPU tensor's -1 never is."""
+    if not (t.is_cuda if at is None else t.get_device() == at) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor on {_place(at)}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must have dtype {dtype}")
+    return t
+
+
+def _device_of(t, name):
+    at = t.get_device()
+    if at < 0:
+        raise ValueError(f"{name} must be on the GPU")
+    return at
+
+
+def _mask(token_mask, T, at):
     import torch
 
     if token_mask is None:
         return None
-    _dev(token_mask, "token_mask")
+    _beside(token_mask, "token_mask", at)
     if token_mask.dtype not in (torch.uint8, torch.bool) or token_mask.numel() != T:
         raise ValueError("token_mask must be uint8 or bool [T]")
     return token_mask.data_ptr()
 
 
-def _sequences(seq_offsets):
+def _sequences(seq_offsets, at):
     import torch
 
     if seq_offsets is None:
         return None, 1
-    _dev(seq_offsets, "seq_offsets", torch.int64)
+    _beside(seq_offsets, "seq_offsets", at, torch.int64)
     if seq_offsets.dim() != 1 or seq_offsets.numel() < 2:
         raise ValueError("seq_offsets must be int64 [S+1]")
     return seq_offsets.data_ptr(), seq_offsets.numel() - 1
 
 
-def _address(t, name, dtype, shape):
-    """The address of a contiguous GPU tensor of that type and shape."""
-    if not (t.is_cuda and t.is_contiguous()) or t.dtype is not dtype or t.shape != shape:
-        raise ValueError(f"{name} must be a contiguous GPU tensor of {dtype} {tuple(shape)}")
+def _address(t, name, dtype, shape, at):
+    """The address of a contiguous tensor of that type and shape on device `at`."""
+    if t.get_device() != at or not t.is_contiguous() or t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name} must be a contiguous tensor of {dtype} {tuple(shape)} on {_place(at)}")
     return t.data_ptr()
 
 
-def _ids(topk_idx, T, k):
+def _ids(topk_idx, T, k, at):
     """The address and the type of expert ids [T,k]."""
     kind = _idx_dtype(topk_idx)
-    return _address(topk_idx, "topk_idx", topk_idx.dtype, (T, k)), kind
+    return _address(topk_idx, "topk_idx", topk_idx.dtype, (T, k), at), kind
 
 
 def grouter_route(scores, k, gating, topk_idx, gate_w, token_mask=None, stream=None):
@@ -524,9 +544,10 @@ def grouter_route(scores, k, gating, topk_idx, gate_w, token_mask=None, stream=N
 
     ld = _matrix(scores, "scores")
     T, E = scores.shape
-    ids, kind = _ids(topk_idx, T, k)
-    gates = _address(gate_w, "gate_w", torch.bfloat16, (T, k))
-    _check(lib().grouter_route(scores.data_ptr(), _float_dtype(scores, "scores"), ld, T, E, k, gating, _mask(token_mask, T), ids, kind, gates,
+    at = scores.get_device()
+    ids, kind = _ids(topk_idx, T, k, at)
+    gates = _address(gate_w, "gate_w", torch.bfloat16, (T, k), at)
+    _check(lib().grouter_route(scores.data_ptr(), _float_dtype(scores, "scores"), ld, T, E, k, gating, _mask(token_mask, T, at), ids, kind, gates,
                                _stream_for(scores, stream)), "grouter_route")
 
 
@@ -534,20 +555,21 @@ def grouter_route_bwd(scores, gating, dscores, topk_idx=None, dlog_gate=None, to
     """dscores [T,E] = gradient out of dlog_gate fp32 [T,k] at topk_idx and/or of the balance loss whose coef fp32 [S,E] is given."""
     import torch
 
-    ld, dld = _matrix(scores, "scores"), _matrix(dscores, "dscores")
+    ld, at = _matrix(scores, "scores"), scores.get_device()
+    dld = _matrix(dscores, "dscores", at)
     T, E = shape = scores.shape
     if dscores.shape != shape:
         raise ValueError("shape mismatch")
     off = ids = dlog = weights = None
     S, k, kind = 1, 0, 0
     if coef is not None:
-        off, S = _sequences(seq_offsets)
-        weights = _address(coef, "coef", torch.float32, (S, E))
+        off, S = _sequences(seq_offsets, at)
+        weights = _address(coef, "coef", torch.float32, (S, E), at)
     if dlog_gate is not None:
         k = dlog_gate.shape[-1]
-        ids, kind = _ids(topk_idx, T, k)
-        dlog = _address(dlog_gate, "dlog_gate", torch.float32, (T, k))
-    _check(lib().grouter_route_bwd(scores.data_ptr(), _float_dtype(scores, "scores"), ld, T, E, gating, _mask(token_mask, T), ids, kind, k, dlog, off, S,
+        ids, kind = _ids(topk_idx, T, k, at)
+        dlog = _address(dlog_gate, "dlog_gate", torch.float32, (T, k), at)
+    _check(lib().grouter_route_bwd(scores.data_ptr(), _float_dtype(scores, "scores"), ld, T, E, gating, _mask(token_mask, T, at), ids, kind, k, dlog, off, S,
                                    weights, dscores.data_ptr(), _float_dtype(dscores, "dscores"), dld, _stream_for(scores, stream)), "grouter_route_bwd")
 
 
@@ -561,15 +583,17 @@ def grouter_balance(scores, gating, topk_idx, alpha, counts, prob, coef, loss, w
 
     ld = _matrix(scores, "scores")
     T, E = scores.shape
-    off, S = _sequences(seq_offsets)
+    at = scores.get_device()
+    off, S = _sequences(seq_offsets, at)
     k = topk_idx.shape[-1]
-    ids, kind = _ids(topk_idx, T, k)
+    ids, kind = _ids(topk_idx, T, k, at)
     fp32, per_sequence = torch.float32, (S, E)
     if not loss.numel() == 1:
         raise ValueError("loss must have one element")
-    _check(lib().grouter_balance(scores.data_ptr(), _float_dtype(scores, "scores"), ld, T, E, k, gating, _mask(token_mask, T), ids, kind, off, S, alpha,
-                                 _address(counts, "counts", torch.int32, per_sequence), _address(prob, "prob", fp32, per_sequence),
-                                 _address(coef, "coef", fp32, per_sequence), _dev(loss, "loss", fp32).data_ptr(), _dev(ws, "ws").data_ptr(),
+    _check(lib().grouter_balance(scores.data_ptr(), _float_dtype(scores, "scores"), ld, T, E, k, gating, _mask(token_mask, T, at), ids, kind, off, S, alpha,
+                                 _address(counts, "counts", torch.int32, per_sequence, at), _address(prob, "prob", fp32, per_sequence, at),
+                                 _address(coef, "coef", fp32, per_sequence, at), _beside(loss, "loss", at, fp32).data_ptr(),
+                                 _beside(ws, "ws", at).data_ptr(),
                                  ws.numel() * ws.element_size(), _stream_for(scores, stream)), "grouter_balance")
 
 
@@ -578,10 +602,11 @@ def grouter_gate_bwd(plan_ws, T, k, E, dY, inp, dlog_gate, stream=None):
     import torch
 
     bf, d = torch.bfloat16, dY.shape[-1]
-    if _dev(plan_ws, "plan_ws").numel() < grouter_plan_bytes(T, k, E):
+    at = _device_of(dY, "dY")
+    if _beside(plan_ws, "plan_ws", at).numel() < grouter_plan_bytes(T, k, E):
         raise ValueError("plan_ws is smaller than a plan of this size")
-    _check(lib().grouter_gate_bwd(plan_ws.data_ptr(), T, k, E, d, _address(dY, "dY", bf, (T, d)), _address(inp, "in", bf, (T * k, d)),
-                                  _address(dlog_gate, "dlog_gate", torch.float32, (T, k)), _stream_for(dY, stream)), "grouter_gate_bwd")
+    _check(lib().grouter_gate_bwd(plan_ws.data_ptr(), T, k, E, d, _address(dY, "dY", bf, (T, d), at), _address(inp, "in", bf, (T * k, d), at),
+                                  _address(dlog_gate, "dlog_gate", torch.float32, (T, k), at), _stream_for(dY, stream)), "grouter_gate_bwd")
 
 
 def grouter_moe_gate_bwd(plan_ws, E, f, dY, ctx_ws, dlog_gate, stream=None):
@@ -590,10 +615,12 @@ def grouter_moe_gate_bwd(plan_ws, E, f, dY, ctx_ws, dlog_gate, stream=None):
 
     T, k = dlog_gate.shape
     d = dY.shape[-1]
-    if _dev(plan_ws, "plan_ws").numel() < grouter_plan_bytes(T, k, E):
+    at = _device_of(dY, "dY")
+    if _beside(plan_ws, "plan_ws", at).numel() < grouter_plan_bytes(T, k, E):
         raise ValueError("plan_ws is smaller than a plan of this size")
-    _check(lib().grouter_moe_gate_bwd(plan_ws.data_ptr(), T, k, E, d, f, _address(dY, "dY", torch.bfloat16, (T, d)), _dev(ctx_ws, "ctx_ws").data_ptr(),
-                                      ctx_ws.numel(), _address(dlog_gate, "dlog_gate", torch.float32, (T, k)), _stream_for(dY, stream)),
+    _check(lib().grouter_moe_gate_bwd(plan_ws.data_ptr(), T, k, E, d, f, _address(dY, "dY", torch.bfloat16, (T, d), at),
+                                      _beside(ctx_ws, "ctx_ws", at).data_ptr(), ctx_ws.numel(),
+                                      _address(dlog_gate, "dlog_gate", torch.float32, (T, k), at), _stream_for(dY, stream)),
            "grouter_moe_gate_bwd")
 
 
@@ -659,9 +686,10 @@ def grouter_adamw(tensors, hyper, grad_scale=None, stream=None):
     import torch
 
     host = isinstance(hyper, AdamWHyper)
-    if not host and _dev(hyper, "hyper", torch.uint8).numel() < ctypes.sizeof(AdamWHyper):
+    at = tensors._held[0][0].get_device() if tensors.count else None
+    if not host and _beside(hyper, "hyper", at, torch.uint8).numel() < ctypes.sizeof(AdamWHyper):
         raise ValueError("hyper must hold 48 bytes")
-    if grad_scale is not None and _dev(grad_scale, "grad_scale", torch.float32).numel() != 1:
+    if grad_scale is not None and _beside(grad_scale, "grad_scale", at, torch.float32).numel() != 1:
         raise ValueError("grad_scale must have one element")
     if not tensors.count:
         return
