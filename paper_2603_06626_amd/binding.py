@@ -566,6 +566,8 @@ def grouter_route_bwd(scores, gating, dscores, topk_idx=None, dlog_gate=None, to
         off, S = _sequences(seq_offsets, at)
         weights = _address(coef, "coef", torch.float32, (S, E), at)
     if dlog_gate is not None:
+        if topk_idx is None:
+            raise ValueError("dlog_gate comes with the topk_idx that it belongs to")
         k = dlog_gate.shape[-1]
         ids, kind = _ids(topk_idx, T, k, at)
         dlog = _address(dlog_gate, "dlog_gate", torch.float32, (T, k), at)

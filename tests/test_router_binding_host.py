@@ -107,3 +107,9 @@ def test_all_on_another_device_than_the_current_one(calls, name):
         getattr(b, name)(**args)
     getattr(b, name)(**args, stream=types.SimpleNamespace(device=types.SimpleNamespace(index=1), cuda_stream=5))
     assert calls[0][1][-1] == 5 and len(calls) == 1
+
+
+def test_gradients_of_gates_without_their_ids(calls):
+    with pytest.raises(ValueError):
+        b.grouter_route_bwd(Fake((T, E), F32), 0, Fake((T, E), F32), dlog_gate=Fake((T, k), F32))
+    assert not calls
