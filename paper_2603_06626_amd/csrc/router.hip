@@ -450,7 +450,7 @@ hipError_t launch_route(const void* scores, int dtype, int64_t ld, int64_t T, in
                 // the tokens with E = 512 37 / 43 and 52 / 43, with E = 1024 74 / 92 and 100 / 91; fp32, E = 1024 138 / 131 and 200 / 127.
                 if (k <= 16 && (dtype == 0 || E <= 256 || k > 12))
                     hipLaunchKernelGGL((k_route_lists<Type, L, V, FULL, 16>), grid, threads, 0, s, x, ld, T, E, k, gating, token_mask, out);
-                else
+                else if constexpr (L > 1)     // (up to 16 experts always have lists)
                     hipLaunchKernelGGL((k_route_rounds<Type, L, V, FULL>), grid, threads, tokens * k * sizeof(uint16_t), s, x, ld, T, E, k, gating,
                                        token_mask, out);
             }
