@@ -637,7 +637,9 @@ class AdamWTensors:
     """The tensors of an optimizer step, looked over once: lists of parameters, gradients and moments of one type each.
 
     param fp32, or bf16, alone or with fp32 `master` copies; grad fp32 or bf16; m and v fp32, or uint8 codes with uint8 exponents
-    m_exp and v_exp of ceil(n/32) elements.  The object holds the tensors; a gradient that moves needs a new one.
+    m_exp and v_exp of ceil(n/32) elements.  The object holds the tensors; a gradient that moves needs a new one, which costs the host about
+    5 us per tensor (12 tensors 60 us, 75 330, 300 1300), more than most steps: keep gradients in place, as this library's own calls do
+    and as autograd does after zero_grad(set_to_none=False).
     """
 
     def __init__(self, param, grad, m, v, master=None, m_exp=None, v_exp=None):
