@@ -2,8 +2,9 @@
 //   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  w = w - (lr wd w + lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)).
 //
 // A pass over memory and little else: 22 to 30 bytes per element with 32-bit moments, 10 to 18 with 8-bit ones.  554 M elements with fp32
-// masters and moments and bf16 gradients 2.88 ms (5.4 TB/s; a large copy reaches 4.8), in bf16 with 8-bit moments 1.02 to 1.07 ms (5.2 to
-// 5.5 TB/s, with the vector units nearly as busy as the memory).  A launch takes the
+// masters and moments and bf16 gradients 2.88 ms (5.4 TB/s; a large copy reaches 4.8), in bf16 with 8-bit moments 1.04 to 1.06 ms (5.3 to
+// 5.4 TB/s; 1.07 to 1.12 ms in a kernel trace), where 606 vector instructions per wave take as long by count: 4 cycles each, 1056 waves per
+// SIMD, 1.07 ms at 2.4 GHz.  A launch takes the
 // addresses of up to kAdamwPerLaunch tensors in its arguments (nothing to copy to the device first, and a graph holds them by value);
 // its workgroups are dealt to the tensors by size.
 //

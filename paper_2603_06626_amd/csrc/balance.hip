@@ -12,8 +12,11 @@ namespace {
 // coef_e = alpha E f_e / n.  The tokens are cut into chunks of equal length, one per workgroup; the part of a sequence inside a chunk
 // leaves its sums in a slot of its own, chunk + sequence (both only grow along the tokens, so no two parts share one), and a second
 // launch adds up each sequence's slots in order.  So work is even whatever the sequences' lengths, and no float is added atomically.
-// Bound by reading where fp32 scores are many (131072 x 256: 27 us, 5 TB/s, and 6 for the join), by exponentials with bf16 ones (21), by the chain of loads, barrier and
-// second launch where they are few (30011 x 60 bf16 in 48 sequences: 7.5 us and 6.2 for the join).
+// 131072 x 256 in fp32 with the scores from memory: 34 us, 4.0 TB/s, what torch's sum over 4 GiB reads, and 6 for the join; over and over on one
+// batch, most of which the last-level cache holds, the two take 28 to 33.  In bf16 24.8 us, 2.7 TB/s: neither reading nor the vector instructions
+// (3891 per wave, 13 us by count, 16 with the exponentials' further cycles) fill it, but two waves per SIMD that load, sum across lanes
+// and count in turn.  Where scores are few it is the chain of loads, barrier and second launch (30011 x 60 bf16 in 48 sequences: 7.3 us
+// and 6.2 for the join).  The figures at the choices below are of passes over and over on one batch.
 struct BalanceCell {
     float prob;
     int32_t count;
